@@ -277,6 +277,44 @@ int hanayo_chunk_adam_step(const hanayo_adam* o, const hanayo_chunk_desc* d, voi
                            float* m, float* v, void* hip_stream);
 
 /* ------------------------------------------------------------------------- *
+ * The norm of all gradients together, and clipping.  For the flush of an iteration: the squared norm of what a
+ * rank holds (hanayo_op_grad_sumsq), the other ranks' numbers next to it or added to it by the caller, then
+ * the gradients scaled down where the norm is too large, in a pass of their own (hanayo_op_grad_clip) or inside
+ * the update (hanayo_adam_step_clipped, hanayo_chunk_adam_step_clipped), which saves that pass.  Nothing waits
+ * for the device.
+ *   norm = sqrt(sumsq[0] + .. + sumsq[parts - 1]);  scale = norm > max_norm ? max_norm / norm : 1
+ * Squares are formed and added in 64 bits, so no fp32 gradient is too large or too small for them; the order is fixed and
+ * results repeat bit for bit.  A norm that is infinite or NaN (a gradient was): hanayo_op_grad_clip takes scale
+ * = 1, and the clipped updates leave parameters and moments as they are; either way `norm` shows it.  (A finite
+ * norm beyond fp32's range, 3.4e38, is infinite in `norm` alone.)
+ * ------------------------------------------------------------------------- */
+typedef struct hanayo_grad {
+  const void* grad; /* device, fp32 or bf16, on an element's boundary; may be NULL if count is 0 */
+  void* out;        /* hanayo_op_grad_clip: where the scaled tensor goes; NULL = in place; equal to grad or apart from it */
+  size_t count;     /* elements, contiguous; may be 0.  All tensors of a call together: at most 2^40 */
+  int dtype;        /* HANAYO_FP32 / HANAYO_BF16, of grad and out */
+} hanayo_grad;
+/* Workspace of hanayo_op_grad_sumsq for a list of n tensors.  Calls that may overlap need one each; nothing has to be cleared. */
+size_t hanayo_op_grad_workspace_bytes(size_t n);
+/* sumsq  device double [1], written: the sum of the squares of all elements of all n tensors (0 without any)
+   grads  host, read during the call only */
+int hanayo_op_grad_sumsq(const hanayo_grad* grads, size_t n, double* sumsq, void* workspace, void* hip_stream);
+typedef struct hanayo_clip {
+  const double* sumsq; /* device double [parts]: the squared norms of `parts` ranks' gradients */
+  int parts;           /* 1 where the caller has added them up already */
+  float max_norm;      /* >= 0; infinity never scales */
+  float* norm;         /* device float [1], written: the norm before clipping (infinite where fp32 ends); may be NULL */
+} hanayo_clip;
+/* out = grad * scale for every tensor, rounded once to its type.  Where scale is 1, tensors in place are left alone. */
+int hanayo_op_grad_clip(const hanayo_grad* grads, size_t n, const hanayo_clip* clip, void* hip_stream);
+/* hanayo_adam_step and hanayo_chunk_adam_step with grads * scale for grads (the gradients themselves are left as they are,
+   or cleared with zero_grads). */
+int hanayo_adam_step_clipped(const hanayo_adam* o, const hanayo_clip* clip, int dtype, void* params, float* master,
+                             float* grads, float* m, float* v, size_t count, void* hip_stream);
+int hanayo_chunk_adam_step_clipped(const hanayo_adam* o, const hanayo_clip* clip, const hanayo_chunk_desc* d, void* weights,
+                                   float* master, float* grads, float* m, float* v, void* hip_stream);
+
+/* ------------------------------------------------------------------------- *
  * Per-rank task executor (the worker-side interpreter of the runtime section,
  * compute actions only).  Runs `list` in order (on one stream unless lanes
  * are asked for, see below).  All chunks of
@@ -633,6 +671,70 @@ int hanayo_op_layernorm_backward_static(int dtype, const void* dout, const void*
                                         int rows, int hidden, void* hip_stream);
 /* out[n] (fp32) += sum over rows of in[row][n].  scratch: at least 64 * n floats. */
 int hanayo_op_colsum_add(int dtype, const void* in, int rows, int n, float* out, float* scratch, void* hip_stream);
+
+/*
+ * Embedding lookup with a scale (sqrt(hidden) in models that scale their embeddings), without a position table:
+ *   out[t][:] = scale * table[tokens[t]][:]
+ * and its gradient, whose rows are first sorted by token, so that however often a token occurs its rows are read by many
+ * wavefronts, and added in a fixed order without atomics:
+ *   d_table[v][:] = (accumulate ? d_table[v][:] : 0) + scale * sum of dout[t][:] over the rows t with tokens[t] = v
+ *   tokens   device int32 [rows]; a token outside [0, vocab) gives a row of zeros, and its row of dout is not read
+ *   table    device [vocab][hidden] storage type;  d_table fp32, added to or (accumulate = 0) written whole: what
+ *            the first micro-batch of an iteration uses, in place of clearing the table
+ *   rows     0 .. 2^24;  hidden a multiple of 8, at most 65536;  row tensors and workspace on 16-byte boundaries
+ *   workspace  device, hanayo_op_embedding_workspace_bytes(); calls that may overlap need one each; nothing to clear
+ */
+int hanayo_op_embedding_forward(int dtype, const void* table, const int32_t* tokens, float scale, void* out, int rows,
+                                int hidden, int vocab, void* hip_stream);
+size_t hanayo_op_embedding_workspace_bytes(int rows, int hidden, int vocab); /* 0 on bad sizes */
+int hanayo_op_embedding_backward(int dtype, const int32_t* tokens, const void* dout, float scale, float* d_table, int rows,
+                                 int hidden, int vocab, int accumulate, void* workspace, void* hip_stream);
+
+/*
+ * The join between two sub-layers of a residual stack: the norm behind a sub-layer, its gate, the residual sum and the norm in
+ * front of the next sub-layer, in one pass over the rows.
+ *   u = Npost(branch);   x_out = x_scale * x + branch_scale * gate * u;   h = Npre(x_out)
+ * N over the last dimension: HANAYO_NORM_LAYER (v - mean) / sqrt(var + eps) * gamma + beta, HANAYO_NORM_RMS
+ * v / sqrt(mean(v^2) + eps) * gamma, HANAYO_NORM_NONE nothing.
+ */
+enum { HANAYO_NORM_NONE = 0, HANAYO_NORM_LAYER = 1, HANAYO_NORM_RMS = 2 };
+enum { HANAYO_GATE_NONE = 0, HANAYO_GATE_CHANNEL = 1, HANAYO_GATE_ELEMENT = 2 };
+typedef struct hanayo_residual_desc {
+  int rows;      /* >= 0 */
+  int hidden;    /* H; multiple of 8, at most 4096 */
+  int dtype;     /* of all row tensors, parameters and the gate */
+  int post_norm; /* HANAYO_NORM_* behind the sub-layer */
+  int pre_norm;  /* HANAYO_NORM_* in front of the next one; HANAYO_NORM_NONE: there is no h */
+  int gate;      /* HANAYO_GATE_*: none, one number per channel [H], or one per element [rows][H] */
+  float x_scale, branch_scale;
+  float eps;     /* > 0 */
+} hanayo_residual_desc;
+/*
+ *   x, branch  device [rows][H] (read);  gate  device [H] or [rows][H], NULL without one
+ *   post, pre  device [2][H] (gamma, beta) for LayerNorm, [H] for RMSNorm, NULL for none
+ *   x_out      device [rows][H], written; may be x, no other two tensors may overlap
+ *   h          device [rows][H], written (NULL without pre_norm); formed from x_out before it is rounded
+ *   stats      device float [rows][4], written for backward: mean and reciprocal deviation of the post-norm, then
+ *              of the pre-norm (mean 0 for RMSNorm; 0 and 1 for no norm); NULL where there is no backward
+ * All on 16-byte boundaries.
+ */
+int hanayo_op_residual_forward(const hanayo_residual_desc* d, const void* x, const void* branch, const void* gate,
+                               const void* post, const void* pre, void* x_out, void* h, float* stats, void* hip_stream);
+/*
+ *   dh         device [rows][H], gradient w.r.t. h (NULL without pre_norm)
+ *   dx_out     device [rows][H], gradient that reaches x_out from elsewhere; NULL = none (with pre_norm only)
+ *   dx, dbranch  device [rows][H], written; dx may be dx_out, no other two tensors may overlap
+ *   dgate      per channel: fp32 [H]; per element: storage type [rows][H], written; NULL without a gate
+ *   d_post, d_pre  fp32, as post and pre (NULL where those are)
+ *   accumulate 1: dgate per channel, d_post and d_pre are added to (and have to hold numbers); 0: they are written
+ *   scratch    device, hanayo_op_residual_scratch_bytes(); calls that may overlap need one each; nothing to clear
+ * Column sums are added in a fixed order without atomics.
+ */
+size_t hanayo_op_residual_scratch_bytes(const hanayo_residual_desc* d); /* 0 on a bad descriptor */
+int hanayo_op_residual_backward(const hanayo_residual_desc* d, const void* x_out, const void* branch, const void* gate,
+                                const void* post, const void* pre, const float* stats, const void* dh, const void* dx_out,
+                                void* dx, void* dbranch, void* dgate, float* d_post, float* d_pre, int accumulate,
+                                void* scratch, void* hip_stream);
 
 /* qkv [b*s][3H] (Q | K | V), ctx [b*s][H], lse [b][heads][s] fp32 (log-sum-exp of the
    scaled, masked scores).  Backward reads qkv, ctx, lse, dctx and writes all of

@@ -9,7 +9,8 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libhanayo.so")
 
 SOURCES = [
-    "schedule.cpp", "layout.cpp", "chunk.cpp", "executor.cpp", "ops.cpp", "ends.cpp", "kernels_ends.hip",
+    "schedule.cpp", "layout.cpp", "chunk.cpp", "executor.cpp", "ops.cpp", "ends.cpp", "train_ops.cpp", "kernels_ends.hip",
+    "kernels_embedding.hip", "kernels_residual.hip", "kernels_grad.hip",
     "kernels_norm.hip", "kernels_generic.hip", "kernels_gemm_dma.hip", "kernels_gemm_wave.hip",
     "kernels_attn_mfma.hip", "kernels_attn_split.hip", "kernels_attn_f32.hip",
 ]

@@ -160,14 +160,19 @@ int head_loss(const Shape& sh, const hanayo_ends_desc* e, const void* lnf, const
   return HANAYO_OK;
 }
 
-int chunk_adam_step(const hanayo_adam* o, const Shape& sh, void* weights, float* master, float* grads, float* m,
-                    float* v, hipStream_t st) {
-  const ParamOffsets po = param_offsets(sh);
+k::AdamArgs adam_args(const hanayo_adam* o, void* params, float* master, float* grads, float* m, float* v, size_t count) {
   k::AdamArgs a{};
-  a.params = weights; a.master = master; a.grads = grads; a.m = m; a.v = v;
-  a.count = po.block_elems * sh.nb;
+  a.params = params; a.master = master; a.grads = grads; a.m = m; a.v = v; a.count = count;
   a.lr = o->lr; a.beta1 = o->beta1; a.beta2 = o->beta2; a.eps = o->eps; a.weight_decay = o->weight_decay;
   a.step = o->step; a.zero_grads = o->zero_grads;
+  return a;
+}
+
+int chunk_adam_step(const hanayo_adam* o, const Shape& sh, void* weights, float* master, float* grads, float* m,
+                    float* v, hipStream_t st, const k::ClipArgs* clip) {
+  const ParamOffsets po = param_offsets(sh);
+  k::AdamArgs a = adam_args(o, weights, master, grads, m, v, po.block_elems * sh.nb);
+  if (clip) a.clip = *clip;
   a.block_elems = po.block_elems;
   static const int kMatrices[4] = {2, 4, 8, 10};  // Wqkv, Wo, W1, W2: the biases and LayerNorm parameters do not decay
   for (int r = 0; r < 4; ++r) {
@@ -232,12 +237,7 @@ int hanayo_adam_step(const hanayo_adam* o, int dtype, void* params, float* maste
   if (!o) return set_error(HANAYO_EINVAL, "adam_step: NULL argument");
   if (dtype != HANAYO_FP32 && dtype != HANAYO_BF16) return set_error(HANAYO_EINVAL, "adam_step: dtype %d", dtype);
   TRY(device_ok());
-  k::AdamArgs a{};
-  a.params = params; a.master = master; a.grads = grads; a.m = m; a.v = v; a.count = count;
-  a.lr = o->lr; a.beta1 = o->beta1; a.beta2 = o->beta2; a.eps = o->eps; a.weight_decay = o->weight_decay;
-  a.step = o->step; a.zero_grads = o->zero_grads;
-  a.block_elems = 0;
-  return k::adam(dtype, a, static_cast<hipStream_t>(hip_stream));
+  return k::adam(dtype, adam_args(o, params, master, grads, m, v, count), static_cast<hipStream_t>(hip_stream));
 }
 
 int hanayo_chunk_adam_step(const hanayo_adam* o, const hanayo_chunk_desc* d, void* weights, float* master, float* grads,

@@ -5,6 +5,7 @@
 #include <hip/hip_runtime.h>
 
 #include "internal.h"
+#include "kernels.h"
 
 namespace hanayo {
 
@@ -20,7 +21,9 @@ int embed_backward(const Shape& sh, const hanayo_ends_desc* e, const int32_t* to
 int head_loss(const Shape& sh, const hanayo_ends_desc* e, const void* lnf, const void* head, const void* y,
               const int32_t* labels, float loss_scale, float* loss, void* dy, float* d_lnf, float* d_head,
               void* workspace, hipStream_t st);
+// clip: nullptr, or the limit that the gradients are scaled down to on the way
 int chunk_adam_step(const hanayo_adam* o, const Shape& sh, void* weights, float* master, float* grads, float* m,
-                    float* v, hipStream_t st);
+                    float* v, hipStream_t st, const k::ClipArgs* clip = nullptr);
+k::AdamArgs adam_args(const hanayo_adam* o, void* params, float* master, float* grads, float* m, float* v, size_t count);
 
 }  // namespace hanayo

@@ -193,6 +193,13 @@ int gather_labelled(int dtype, const int32_t* labels, const void* in, int rows, 
 // rows' negative log-likelihoods); nll[i] = the row's negative log-likelihood.
 int softmax_xent(int dtype, void* logits, const int32_t* labels, const int* live, const int32_t* list, float loss_scale,
                  float* nll, int rows, int V, hipStream_t stream);
+// The limit that gradients are scaled down to (see clip.h); device pointers.
+struct ClipArgs {
+  const double* sumsq;  // [parts] squared norms of the ranks' gradients; nullptr: no clipping
+  int parts;
+  float max_norm;
+  float* norm;  // [1] written: the norm before clipping; may be nullptr
+};
 struct AdamArgs {
   void* params;   // storage type, updated
   float* master;  // bf16 storage: fp32 copy of the parameters, updated; ignored for fp32 storage
@@ -207,7 +214,9 @@ struct AdamArgs {
   // the four ranges [lo, hi)
   size_t block_elems;
   size_t lo[4], hi[4];
+  ClipArgs clip;
 };
+int adam_check(int dtype, const AdamArgs& a);  // what adam refuses, without touching the GPU
 int adam(int dtype, const AdamArgs& a, hipStream_t stream);
 
 // out[row][:] = row slot[row] of the [live][H] product (zeros where slot is -1).  grid > 0: the product is the sum of the
@@ -215,6 +224,43 @@ int adam(int dtype, const AdamArgs& a, hipStream_t stream);
 // Also loss[0] = sum(nll[0..live)) / live (0 if live is 0).
 int scatter_rows(int dtype, const void* product, const int* live, const int32_t* slot, int grid, int K, void* out, int rows, int H,
                  const float* nll, float* loss, hipStream_t stream);
+
+// ---- gradient norm and clipping over many tensors ------------------------------
+constexpr size_t kGradMaxElements = (size_t)1 << 40;  // of all tensors of a call
+size_t grad_workspace_bytes(size_t n);
+// sumsq[0] = sum of the squares of all elements
+int grad_sumsq(const hanayo_grad* grads, size_t n, double* sumsq, double* workspace, hipStream_t stream);
+// out = grad * scale (out nullptr: in place)
+int grad_clip(const hanayo_grad* grads, size_t n, const ClipArgs& clip, hipStream_t stream);
+
+// ---- embedding with a scale -------------------------------------------------------
+// out[t][:] = scale * table[token[t]][:], zeros for a token outside [0, vocab)
+int embedding_forward(int dtype, const void* table, const int32_t* tokens, float scale, void* out, int rows, int H, int vocab,
+                      hipStream_t stream);
+// d_table[v][:] (+)= scale * sum of the rows of dout that hold token v
+constexpr int kEmbeddingMaxRows = 1 << 24;
+size_t embedding_workspace_bytes(int rows, int H);
+int embedding_backward(int dtype, const int32_t* tokens, const void* dout, float scale, float* d_table, int rows, int H, int vocab,
+                       bool accumulate, void* workspace, hipStream_t stream);
+
+// ---- residual join: norms after one sub-layer and before the next -----------------
+constexpr int kResidualMaxHidden = 4096;
+struct ResidualArgs {
+  int rows, H, post, pre, gate_kind;
+  float x_scale, branch_scale, eps;
+  const void *x, *branch, *gate, *w_post, *w_pre;
+  void *x_out, *h;
+  float4* stats;  // (post mean, post rstd, pre mean, pre rstd) per row
+  // backward
+  const void *dh, *dx_out;
+  void *dx, *dbranch, *dgate;
+  float *d_post, *d_pre;
+  bool accumulate;
+  float* scratch;
+};
+int residual_forward(int dtype, const ResidualArgs& a, hipStream_t stream);
+size_t residual_scratch_bytes(int rows, int H);
+int residual_backward(int dtype, const ResidualArgs& a, hipStream_t stream);
 
 // ---- misc ------------------------------------------------------------------------
 // max_workgroups > 0 caps the grid: a copy that uses only a few CUs and so runs at a chosen fraction of the

@@ -5,6 +5,7 @@
 // (embedding) or one workgroup (a vocabulary row) per row.
 #include <cmath>
 
+#include "clip.h"
 #include "device_util.h"
 #include "kernels.h"
 
@@ -396,12 +397,12 @@ struct AdamDev {
   // the four [lo, hi) ranges
   size_t block_elems;
   size_t lo[4], hi[4];
+  ClipArgs clip;
 };
 
-template <typename T>
-__global__ __launch_bounds__(256) void adam_kernel(AdamDev a) {
-  const size_t i = ((size_t)blockIdx.x * 256 + threadIdx.x) * 4;
-  if (i >= a.count) return;
+// One vector of the four arrays, the gradient scaled by `scale` first where CLIP is set.
+template <typename T, bool CLIP>
+__device__ __forceinline__ void adam_vector(const AdamDev& a, size_t i, float scale) {
   bool decay = true;
   if (a.block_elems) {
     const size_t pos = i % a.block_elems;
@@ -410,7 +411,11 @@ __global__ __launch_bounds__(256) void adam_kernel(AdamDev a) {
     for (int r = 0; r < 4; ++r) decay = decay || (pos >= a.lo[r] && pos < a.hi[r]);
   }
   const float wd = decay ? a.weight_decay : 0.f;
-  const f32x4 g = *reinterpret_cast<const f32x4*>(a.grads + i);
+  f32x4 g = *reinterpret_cast<const f32x4*>(a.grads + i);
+  if constexpr (CLIP) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) g[e] *= scale;
+  }
   f32x4 m = *reinterpret_cast<const f32x4*>(a.m + i);
   f32x4 v = *reinterpret_cast<const f32x4*>(a.v + i);
   f32x4 p;
@@ -439,6 +444,25 @@ __global__ __launch_bounds__(256) void adam_kernel(AdamDev a) {
     *reinterpret_cast<f32x4*>(static_cast<float*>(a.params) + i) = p;
   }
   if (a.zero_grads) *reinterpret_cast<f32x4*>(a.grads + i) = f32x4{0.f, 0.f, 0.f, 0.f};
+}
+
+template <typename T>
+__global__ __launch_bounds__(256) void adam_kernel(AdamDev a) {
+  const size_t i = ((size_t)blockIdx.x * 256 + threadIdx.x) * 4;
+  if (i < a.count) adam_vector<T, false>(a, i, 1.f);
+}
+
+// With clipping a workgroup forms the factor once and walks the arrays with it.  A norm that is not finite leaves parameters
+// and moments as they are (the gradients are still cleared if they are to be).
+template <typename T>
+__global__ __launch_bounds__(256) void adam_clip_kernel(AdamDev a) {
+  const ClipScale s = clip_scale(a.clip);
+  if (a.clip.norm && blockIdx.x == 0 && threadIdx.x == 0) a.clip.norm[0] = s.norm;
+  const size_t stride = (size_t)gridDim.x * 1024;
+  for (size_t i = ((size_t)blockIdx.x * 256 + threadIdx.x) * 4; i < a.count; i += stride) {
+    if (s.finite) adam_vector<T, true>(a, i, s.scale);
+    else if (a.zero_grads) *reinterpret_cast<f32x4*>(a.grads + i) = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
 }
 
 }  // namespace
@@ -527,12 +551,17 @@ int softmax_xent(int dtype, void* logits, const int32_t* labels, const int* live
   return check_launch("softmax_xent");
 }
 
-int adam(int dtype, const AdamArgs& g, hipStream_t stream) {
+int adam_check(int dtype, const AdamArgs& g) {
   if (!g.params || !g.grads || !g.m || !g.v) return set_error(HANAYO_EINVAL, "adam: NULL argument");
   if (g.count == 0 || g.count % 4) return set_error(HANAYO_EINVAL, "adam: element count %zu is not a positive multiple of 4", g.count);
   if (dtype == HANAYO_BF16 && !g.master) return set_error(HANAYO_EINVAL, "adam: bf16 parameters need an fp32 master copy");
   if (g.step < 1 || !(g.beta1 >= 0.f && g.beta1 < 1.f) || !(g.beta2 >= 0.f && g.beta2 < 1.f))
     return set_error(HANAYO_EINVAL, "adam: step %d beta1 %g beta2 %g", g.step, g.beta1, g.beta2);
+  return HANAYO_OK;
+}
+
+int adam(int dtype, const AdamArgs& g, hipStream_t stream) {
+  if (const int rc = adam_check(dtype, g)) return rc;
   AdamDev a{};
   a.params = g.params; a.master = dtype == HANAYO_BF16 ? g.master : nullptr; a.grads = g.grads; a.m = g.m; a.v = g.v;
   a.count = g.count;
@@ -543,6 +572,13 @@ int adam(int dtype, const AdamArgs& g, hipStream_t stream) {
   a.block_elems = g.block_elems;
   for (int r = 0; r < 4; ++r) a.lo[r] = g.lo[r], a.hi[r] = g.hi[r];
   const size_t vec = g.count / 4, blocks = (vec + 255) / 256;
+  if (g.clip.sumsq) {
+    a.clip = g.clip;
+    const dim3 grid((unsigned)(blocks < 2048 ? blocks : 2048));  // 8 workgroups on every CU
+    if (dtype == HANAYO_BF16) launch_kernel(adam_clip_kernel<bf16>, grid, dim3(256), 0, stream, a);
+    else launch_kernel(adam_clip_kernel<float>, grid, dim3(256), 0, stream, a);
+    return check_launch("adam (clipped)");
+  }
   if (blocks > 0x7fffffffu) return set_error(HANAYO_EUNSUPPORTED, "adam: too many elements");
   if (dtype == HANAYO_BF16) launch_kernel(adam_kernel<bf16>, dim3((unsigned)blocks), dim3(256), 0, stream, a);
   else launch_kernel(adam_kernel<float>, dim3((unsigned)blocks), dim3(256), 0, stream, a);

@@ -96,10 +96,25 @@ class LinkArgs(ctypes.Structure):
                 ("async_", ctypes.c_int), ("link_workgroups", ctypes.c_int)]
 
 
+class ResidualDesc(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int), ("hidden", ctypes.c_int), ("dtype", ctypes.c_int), ("post_norm", ctypes.c_int),
+                ("pre_norm", ctypes.c_int), ("gate", ctypes.c_int), ("x_scale", ctypes.c_float),
+                ("branch_scale", ctypes.c_float), ("eps", ctypes.c_float)]
+
+
+class Grad(ctypes.Structure):
+    _fields_ = [("grad", ctypes.c_void_p), ("out", ctypes.c_void_p), ("count", ctypes.c_size_t), ("dtype", ctypes.c_int)]
+
+
+class Clip(ctypes.Structure):
+    _fields_ = [("sumsq", ctypes.c_void_p), ("parts", ctypes.c_int), ("max_norm", ctypes.c_float), ("norm", ctypes.c_void_p)]
+
+
 class HanayoError(RuntimeError):
-    def __init__(self, code):
+    def __init__(self, code, detail=None):
         self.code = code
-        detail = _lib.hanayo_last_error().decode()
+        if detail is None:
+            detail = _lib.hanayo_last_error().decode()
         super().__init__("%s (%d): %s" % (_lib.hanayo_strerror(code).decode(), code, detail))
 
 
@@ -112,7 +127,11 @@ EXPORTS = ("hanayo_strerror", "hanayo_last_error", "hanayo_stage_rank", "hanayo_
            "hanayo_op_gemm", "hanayo_op_gemm_group", "hanayo_op_gemm_config", "hanayo_op_gemm_kernel", "hanayo_op_copy", "hanayo_op_layernorm_forward", "hanayo_op_layernorm_backward", "hanayo_op_layernorm_backward_static", "hanayo_op_colsum_add",
            "hanayo_op_attention_forward", "hanayo_op_attention_backward",
            "hanayo_embed_forward", "hanayo_embed_backward", "hanayo_head_workspace_bytes", "hanayo_head_loss",
-           "hanayo_adam_step", "hanayo_chunk_adam_step", "hanayo_ends_workspace_bytes")
+           "hanayo_adam_step", "hanayo_chunk_adam_step", "hanayo_ends_workspace_bytes",
+           "hanayo_op_embedding_forward", "hanayo_op_embedding_workspace_bytes", "hanayo_op_embedding_backward",
+           "hanayo_op_residual_forward", "hanayo_op_residual_scratch_bytes", "hanayo_op_residual_backward",
+           "hanayo_op_grad_workspace_bytes", "hanayo_op_grad_sumsq", "hanayo_op_grad_clip", "hanayo_adam_step_clipped",
+           "hanayo_chunk_adam_step_clipped")
 
 _vp, _sz, _int = ctypes.c_void_p, ctypes.c_size_t, ctypes.c_int
 _descp = ctypes.POINTER(ChunkDesc)
@@ -170,6 +189,23 @@ _lib.hanayo_ends_workspace_bytes.argtypes = [_descp, _endsp]
 _lib.hanayo_head_loss.argtypes = [_descp, _endsp, _vp, _vp, _vp, _vp, ctypes.c_float, _vp, _vp, _vp, _vp, _vp, _vp]
 _lib.hanayo_adam_step.argtypes = [_adamp, _int, _vp, _vp, _vp, _vp, _vp, _sz, _vp]
 _lib.hanayo_chunk_adam_step.argtypes = [_adamp, _descp, _vp, _vp, _vp, _vp, _vp, _vp]
+_clipp, _residualp = ctypes.POINTER(Clip), ctypes.POINTER(ResidualDesc)
+_lib.hanayo_op_embedding_forward.argtypes = [_int, _vp, _vp, ctypes.c_float, _vp, _int, _int, _int, _vp]
+_lib.hanayo_op_embedding_workspace_bytes.restype = _sz
+_lib.hanayo_op_embedding_workspace_bytes.argtypes = [_int, _int, _int]
+_lib.hanayo_op_embedding_backward.argtypes = [_int, _vp, _vp, ctypes.c_float, _vp, _int, _int, _int, _int, _vp, _vp]
+_lib.hanayo_op_residual_forward.argtypes = [_residualp] + [_vp] * 9
+_lib.hanayo_op_residual_scratch_bytes.restype = _sz
+_lib.hanayo_op_residual_scratch_bytes.argtypes = [_residualp]
+_lib.hanayo_op_residual_backward.argtypes = [_residualp] + [_vp] * 13 + [_int, _vp, _vp]
+_lib.hanayo_op_grad_workspace_bytes.restype = _sz
+_lib.hanayo_op_grad_workspace_bytes.argtypes = [_sz]
+_lib.hanayo_op_grad_sumsq.argtypes = [_vp, _sz, _vp, _vp, _vp]
+_lib.hanayo_op_grad_clip.argtypes = [_vp, _sz, _clipp, _vp]
+_lib.hanayo_adam_step_clipped.argtypes = [_adamp, _clipp, _int, _vp, _vp, _vp, _vp, _vp, _sz, _vp]
+_lib.hanayo_chunk_adam_step_clipped.argtypes = [_adamp, _clipp, _descp, _vp, _vp, _vp, _vp, _vp, _vp]
+NORM_NONE, NORM_LAYER, NORM_RMS = range(3)
+GATE_NONE, GATE_CHANNEL, GATE_ELEMENT = range(3)
 EPI_NONE, EPI_BIAS, EPI_BIAS_GELU, EPI_BIAS_RES, EPI_MUL_DGELU, EPI_ADD, EPI_ACCUM_F32 = range(7)
 
 
@@ -186,6 +222,21 @@ def _ptr(t):
         return t
     if isinstance(t, np.ndarray):
         return t.ctypes.data
+    return t.data_ptr()
+
+
+def _room(what, t, count, size):
+    """Device address of an operand of `count` elements of `size` bytes: an integer address as it is, None as NULL; a tensor
+    that is not on the current device, not contiguous, of another element size or too small is refused."""
+    if t is None or type(t) is int:
+        return t
+    if not isinstance(t, torch.Tensor) or not t.is_cuda or not t.is_contiguous():
+        raise HanayoError(EINVAL, "%s: a contiguous tensor on the GPU is wanted" % what)
+    if t.element_size() != size or t.numel() < count:
+        raise HanayoError(EINVAL, "%s: %d elements of %d bytes are wanted, not %d of %d"
+                          % (what, count, size, t.numel(), t.element_size()))
+    if t.get_device() != torch.cuda.current_device():
+        raise HanayoError(EINVAL, "%s: the tensor is not on the current device" % what)
     return t.data_ptr()
 
 
@@ -386,6 +437,120 @@ def hanayo_adam_step(adam, dtype, params, master, grads, m, v, count, stream=Non
 def hanayo_chunk_adam_step(adam, desc, weights, master, grads, m, v, stream=None):
     _check(_lib.hanayo_chunk_adam_step(ctypes.byref(adam), ctypes.byref(desc), _ptr(weights), _ptr(master), _ptr(grads),
                                        _ptr(m), _ptr(v), stream))
+
+
+def hanayo_op_embedding_forward(dtype, table, tokens, scale, out, rows, hidden, vocab, stream=None):
+    e = 2 if dtype == BF16 else 4
+    _check(_lib.hanayo_op_embedding_forward(dtype, _room("table", table, vocab * hidden, e), _room("tokens", tokens, rows, 4),
+                                            scale, _room("out", out, rows * hidden, e), rows, hidden, vocab, stream))
+
+
+def hanayo_op_embedding_workspace_bytes(rows, hidden, vocab):
+    v = _lib.hanayo_op_embedding_workspace_bytes(rows, hidden, vocab)
+    if v == 0:
+        raise HanayoError(EINVAL)
+    return v
+
+
+def hanayo_op_embedding_backward(dtype, tokens, dout, scale, d_table, rows, hidden, vocab, accumulate, workspace, stream=None):
+    e = 2 if dtype == BF16 else 4
+    need = _lib.hanayo_op_embedding_workspace_bytes(rows, hidden, vocab)
+    _check(_lib.hanayo_op_embedding_backward(dtype, _room("tokens", tokens, rows, 4), _room("dout", dout, rows * hidden, e), scale,
+                                             _room("d_table", d_table, vocab * hidden, 4), rows, hidden, vocab, int(accumulate),
+                                             _room("workspace", workspace, need, 1), stream))
+
+
+def _residual_sizes(d):
+    """(element size, elements of a row tensor, of the post-norm's and the pre-norm's parameters, of the gate)."""
+    n, H = d.rows * d.hidden, d.hidden
+    return (2 if d.dtype == BF16 else 4, n, 2 * H if d.post_norm == NORM_LAYER else H, 2 * H if d.pre_norm == NORM_LAYER else H,
+            n if d.gate == GATE_ELEMENT else H)
+
+
+def hanayo_op_residual_forward(desc, x, branch, gate, post, pre, x_out, h, stats, stream=None):
+    e, n, n_post, n_pre, n_gate = _residual_sizes(desc)
+    _check(_lib.hanayo_op_residual_forward(
+        ctypes.byref(desc), _room("x", x, n, e), _room("branch", branch, n, e), _room("gate", gate, n_gate, e),
+        _room("post", post, n_post, e), _room("pre", pre, n_pre, e), _room("x_out", x_out, n, e), _room("h", h, n, e),
+        _room("stats", stats, 4 * desc.rows, 4), stream))
+
+
+def hanayo_op_residual_scratch_bytes(desc):
+    v = _lib.hanayo_op_residual_scratch_bytes(ctypes.byref(desc))
+    if v == 0:
+        raise HanayoError(EINVAL)
+    return v
+
+
+def hanayo_op_residual_backward(desc, x_out, branch, gate, post, pre, stats, dh, dx_out, dx, dbranch, dgate, d_post, d_pre,
+                                accumulate, scratch, stream=None):
+    e, n, n_post, n_pre, n_gate = _residual_sizes(desc)
+    need = _lib.hanayo_op_residual_scratch_bytes(ctypes.byref(desc))
+    _check(_lib.hanayo_op_residual_backward(
+        ctypes.byref(desc), _room("x_out", x_out, n, e), _room("branch", branch, n, e), _room("gate", gate, n_gate, e),
+        _room("post", post, n_post, e), _room("pre", pre, n_pre, e), _room("stats", stats, 4 * desc.rows, 4), _room("dh", dh, n, e),
+        _room("dx_out", dx_out, n, e), _room("dx", dx, n, e), _room("dbranch", dbranch, n, e),
+        _room("dgate", dgate, n_gate, e if desc.gate == GATE_ELEMENT else 4), _room("d_post", d_post, n_post, 4),
+        _room("d_pre", d_pre, n_pre, 4), int(accumulate), _room("scratch", scratch, need, 1), stream))
+
+
+class GradList:
+    """The tensors of a model's gradients, as hanayo_op_grad_sumsq and hanayo_op_grad_clip take them: marshalled once, kept
+    for as long as the tensors stay where they are."""
+
+    def __init__(self, grads, outs=None):
+        if outs is not None and len(outs) != len(grads):
+            raise HanayoError(EINVAL, "grad_list: %d tensors, %d outputs" % (len(grads), len(outs)))
+        self.keep = (list(grads), None if outs is None else list(outs))
+        self.array = (Grad * max(1, len(grads)))()
+        for i, g in enumerate(grads):
+            out = None if outs is None else outs[i]
+            if g.dtype not in (torch.float32, torch.bfloat16) or (out is not None and out.dtype != g.dtype):
+                raise HanayoError(EINVAL, "grad_list: tensor %d: fp32 or bf16, and its output of the same type" % i)
+            n, e = g.numel(), g.element_size()
+            self.array[i] = Grad(_room("tensor %d" % i, g, n, e), _room("output %d" % i, out, n, e), n,
+                                 BF16 if g.dtype == torch.bfloat16 else FP32)
+        self.count = len(grads)
+
+
+def grad_list(grads, outs=None):
+    return GradList(grads, outs)
+
+
+def make_clip(sumsq, parts, max_norm, norm=None):
+    c = Clip(_room("sumsq", sumsq, parts, 8), parts, max_norm, _room("norm", norm, 1, 4))
+    c._keep = (sumsq, norm)
+    return c
+
+
+def hanayo_op_grad_workspace_bytes(n):
+    return _lib.hanayo_op_grad_workspace_bytes(n)
+
+
+def hanayo_op_grad_sumsq(grads, sumsq, workspace, stream=None):
+    """grads: a GradList."""
+    need = _lib.hanayo_op_grad_workspace_bytes(grads.count)
+    _check(_lib.hanayo_op_grad_sumsq(ctypes.addressof(grads.array), grads.count, _room("sumsq", sumsq, 1, 8),
+                                     _room("workspace", workspace, need, 1), stream))
+
+
+def hanayo_op_grad_clip(grads, clip, stream=None):
+    """grads: a GradList; clip: of make_clip."""
+    _check(_lib.hanayo_op_grad_clip(ctypes.addressof(grads.array), grads.count, ctypes.byref(clip), stream))
+
+
+def hanayo_adam_step_clipped(adam, clip, dtype, params, master, grads, m, v, count, stream=None):
+    e = 2 if dtype == BF16 else 4
+    _check(_lib.hanayo_adam_step_clipped(ctypes.byref(adam), ctypes.byref(clip), dtype, _room("params", params, count, e),
+                                         _room("master", master, count, 4), _room("grads", grads, count, 4),
+                                         _room("m", m, count, 4), _room("v", v, count, 4), count, stream))
+
+
+def hanayo_chunk_adam_step_clipped(adam, clip, desc, weights, master, grads, m, v, stream=None):
+    n, e = _lib.hanayo_grad_bytes(ctypes.byref(desc)) // 4, 2 if desc.dtype == BF16 else 4
+    _check(_lib.hanayo_chunk_adam_step_clipped(ctypes.byref(adam), ctypes.byref(clip), ctypes.byref(desc),
+                                               _room("weights", weights, n, e), _room("master", master, n, 4),
+                                               _room("grads", grads, n, 4), _room("m", m, n, 4), _room("v", v, n, 4), stream))
 
 
 def hanayo_op_gemm(dtype, A, B, C, M, N, K, lda, ldb, ldc, a_t, b_t, epilogue, bias=None, aux=None, aux_out=None,
