@@ -51,6 +51,18 @@ __device__ __forceinline__ float ld(const bf16* p) { return (float)*p; }
 __device__ __forceinline__ void st(float* p, float v) { *p = v; }
 __device__ __forceinline__ void st(bf16* p, float v) { *p = (bf16)v; }
 
+// A vector of data that passes through once: STREAM = past the caches, so that what will be read again stays in them.
+template <bool STREAM, typename V>
+__device__ __forceinline__ V fetch(const V* p) {
+  if constexpr (STREAM) return __builtin_nontemporal_load(p);
+  else return *p;
+}
+template <bool STREAM, typename V>
+__device__ __forceinline__ void put(V* p, V v) {
+  if constexpr (STREAM) __builtin_nontemporal_store(v, p);
+  else *p = v;
+}
+
 // Butterfly reductions over lanes l ^ 32, l ^ 16, ... l ^ 1 without the LDS crossbar that __shfl_xor goes through (about 100
 // cycles a step): the swaps exchange halves and 16-lane rows between two registers, and inside a row a rotation by 8 is l ^ 8,
 // after which lanes that differ by 8 agree and a rotation by 4 is as good as l ^ 4, and so on.  The same additions in the same

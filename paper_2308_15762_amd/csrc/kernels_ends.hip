@@ -400,7 +400,9 @@ struct AdamDev {
   ClipArgs clip;
 };
 
-// One vector of the four arrays, the gradient scaled by `scale` first where CLIP is set.
+// One vector of the four arrays, the gradient scaled by `scale` first where CLIP is set.  With clipping the arrays pass by the
+// caches (nothing here is read again before the next iteration), which leaves the gradients' first part, kept by the pass that
+// formed their norm, where it is.
 template <typename T, bool CLIP>
 __device__ __forceinline__ void adam_vector(const AdamDev& a, size_t i, float scale) {
   bool decay = true;
@@ -411,16 +413,16 @@ __device__ __forceinline__ void adam_vector(const AdamDev& a, size_t i, float sc
     for (int r = 0; r < 4; ++r) decay = decay || (pos >= a.lo[r] && pos < a.hi[r]);
   }
   const float wd = decay ? a.weight_decay : 0.f;
-  f32x4 g = *reinterpret_cast<const f32x4*>(a.grads + i);
+  f32x4 g = fetch<CLIP>(reinterpret_cast<const f32x4*>(a.grads + i));
   if constexpr (CLIP) {
 #pragma unroll
     for (int e = 0; e < 4; ++e) g[e] *= scale;
   }
-  f32x4 m = *reinterpret_cast<const f32x4*>(a.m + i);
-  f32x4 v = *reinterpret_cast<const f32x4*>(a.v + i);
+  f32x4 m = fetch<CLIP>(reinterpret_cast<const f32x4*>(a.m + i));
+  f32x4 v = fetch<CLIP>(reinterpret_cast<const f32x4*>(a.v + i));
   f32x4 p;
   if (a.master) {
-    p = *reinterpret_cast<const f32x4*>(a.master + i);
+    p = fetch<CLIP>(reinterpret_cast<const f32x4*>(a.master + i));
   } else {
 #pragma unroll
     for (int e = 0; e < 4; ++e) p[e] = ld(static_cast<const T*>(a.params) + i + e);
@@ -432,16 +434,16 @@ __device__ __forceinline__ void adam_vector(const AdamDev& a, size_t i, float sc
     const float mhat = m[e] * a.corr1, vhat = v[e] * a.corr2;
     p[e] = p[e] - a.lr * (mhat / (sqrtf(vhat) + a.eps) + wd * p[e]);
   }
-  *reinterpret_cast<f32x4*>(a.m + i) = m;
-  *reinterpret_cast<f32x4*>(a.v + i) = v;
-  if (a.master) *reinterpret_cast<f32x4*>(a.master + i) = p;
+  put<CLIP>(reinterpret_cast<f32x4*>(a.m + i), m);
+  put<CLIP>(reinterpret_cast<f32x4*>(a.v + i), v);
+  if (a.master) put<CLIP>(reinterpret_cast<f32x4*>(a.master + i), p);
   if constexpr (sizeof(T) == 2) {
     bf16x4 o;
 #pragma unroll
     for (int e = 0; e < 4; ++e) o[e] = (bf16)p[e];
-    *reinterpret_cast<bf16x4*>(static_cast<bf16*>(a.params) + i) = o;
+    put<CLIP>(reinterpret_cast<bf16x4*>(static_cast<bf16*>(a.params) + i), o);
   } else {
-    *reinterpret_cast<f32x4*>(static_cast<float*>(a.params) + i) = p;
+    put<CLIP>(reinterpret_cast<f32x4*>(static_cast<float*>(a.params) + i), p);
   }
   if (a.zero_grads) *reinterpret_cast<f32x4*>(a.grads + i) = f32x4{0.f, 0.f, 0.f, 0.f};
 }

@@ -8,6 +8,8 @@
 // an error far below the fp32 result's last bit; the pass reads 4 bytes per conversion and addition, which the 64-bit rate of the vector
 // units covers many times over.  Tensors are cut into tiles, and a launch's tiles go round its workgroups in turn; which
 // partial sum holds what depends on the sizes alone, and the partial sums are added in order, so results repeat bit for bit.
+#include <type_traits>
+
 #include "clip.h"
 #include "device_util.h"
 #include "kernels.h"
@@ -17,11 +19,17 @@ namespace k {
 
 namespace {
 
-constexpr unsigned kTile = 8192;     // elements of a tile
-constexpr int kMaxBlocks = 2048;     // workgroups of a launch at most: 8 on every CU, one partial sum each
+constexpr unsigned kTileBytes = 32768;  // of a tensor: eight 16-byte loads a thread, all in flight at once
+constexpr int kMaxBlocks = 2048;        // workgroups of a launch at most: 8 on every CU, one partial sum each
+constexpr int kLoads = kTileBytes / 16 / 256;
+// The pass that forms the norm leaves the first 192 MiB of a launch's tensors in the 256 MB cache and reads the rest past it, so that the pass
+// that scales or uses them finds that part there; that pass reads and writes past the cache.  Norm and clipping of 403 MB:
+// 181 us, of 1013 us with Adam on 609 MB (30 bytes an element) 852; with ordinary loads and stores everywhere 238 and 1046, the rest past the
+// cache in the first pass only 200 and 1043, nothing kept 214 and 1013.
+constexpr unsigned kKeepTiles = 192u * (1 << 20) / kTileBytes;
 
 // A launch's tensors.  The table travels in the kernel's arguments: nothing to copy to the device first, so that a call can be
-// captured into a graph, and nothing to keep alive.  Entry `n` holds the number of tiles.
+// captured into a graph, and nothing to keep alive.
 struct GradEntry {
   const void* in;
   void* out;
@@ -36,61 +44,140 @@ struct GradTable {
   unsigned tiles;
 };
 
-// The tensor that holds `tile` (tensors without elements hold none).
-__device__ __forceinline__ int find_tensor(const GradTable& t, unsigned tile) {
-  int lo = 0, hi = t.n - 1;
-  while (lo < hi) {
-    const int mid = (lo + hi + 1) / 2;
-    if (t.e[mid].first <= tile) lo = mid;
-    else hi = mid - 1;
+// Which tensor a tile lies in.  The lanes of a wavefront hold the tensors' first tiles, two each, and vote: one trip to memory
+// for the whole launch in place of one for each step of a search.
+struct TensorFinder {
+  unsigned lo, hi;
+  __device__ __forceinline__ TensorFinder(const GradTable& t) {
+    static_assert(kEntries <= 128, "two tensors a lane");
+    const int lane = threadIdx.x & 63;
+    lo = lane < t.n ? t.e[lane].first : 0xffffffffu;
+    hi = lane + 64 < t.n ? t.e[lane + 64].first : 0xffffffffu;
   }
-  return lo;
+  __device__ __forceinline__ int operator()(unsigned tile) const {
+    return __popcll(__ballot(lo <= tile)) + __popcll(__ballot(hi <= tile)) - 1;
+  }
+};
+
+__device__ __forceinline__ double sum_256(double v, double* red) {  // red: [4]; the same sum in every thread
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, kWave);
+  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
+  __syncthreads();
+  return red[0] + red[1] + red[2] + red[3];
 }
 
-__device__ __forceinline__ double block_sum(double v, double* red) {
-  red[threadIdx.x] = v;
-  __syncthreads();
-  for (int o = 128; o > 0; o >>= 1) {
-    if ((int)threadIdx.x < o) red[threadIdx.x] += red[threadIdx.x + o];
-    __syncthreads();
+// Elements of a tile before its first 16-byte boundary, and whole vectors behind that; a thread takes vector `thread + 256 u`.
+template <typename T>
+struct TileSplit {
+  static constexpr unsigned kVec = 16 / sizeof(T);
+  size_t begin;
+  unsigned n, head, vecs;
+  __device__ __forceinline__ TileSplit(const GradEntry& e, unsigned tile) {
+    constexpr unsigned kTile = kTileBytes / sizeof(T);
+    begin = (size_t)(tile - e.first) * kTile;
+    n = e.count - begin < kTile ? (unsigned)(e.count - begin) : kTile;
+    head = (16u - (unsigned)(reinterpret_cast<uintptr_t>(e.in) & 15u)) % 16u / sizeof(T);  // a tile is a whole number of vectors
+    if (head > n) head = n;
+    vecs = (n - head) / kVec;
   }
-  return red[0];
+  // The elements that belong to no vector: fewer than two vectors' worth, one each for the first threads; n: none.
+  __device__ __forceinline__ unsigned loose(unsigned thread) const {
+    const unsigned i = thread < head ? thread : thread + vecs * kVec;
+    return i < n ? i : n;
+  }
+};
+
+template <typename T, bool KEEP>
+__device__ __forceinline__ double tile_sumsq(const GradEntry& e, unsigned tile) {
+  using Vec = typename std::conditional<sizeof(T) == 2, bf16x8, f32x4>::type;
+  const TileSplit<T> s(e, tile);
+  const T* in = static_cast<const T*>(e.in) + s.begin;
+  double acc = 0.0;
+  if (s.vecs) {  // uniform; loads behind the last vector read it again and count as nothing: no branch between the loads
+    Vec v[kLoads];
+#pragma unroll
+    for (int u = 0; u < kLoads; ++u)
+      v[u] = fetch<!KEEP>(reinterpret_cast<const Vec*>(in + s.head + min(threadIdx.x + 256u * u, s.vecs - 1) * s.kVec));
+#pragma unroll
+    for (int u = 0; u < kLoads; ++u) {
+      double part = 0.0;
+#pragma unroll
+      for (unsigned j = 0; j < s.kVec; ++j) {
+        const double x = (float)v[u][j];
+        part += x * x;
+      }
+      acc += threadIdx.x + 256u * u < s.vecs ? part : 0.0;
+    }
+  }
+  const unsigned i = s.loose(threadIdx.x);
+  if (i < s.n) {
+    const double x = ld(in + i);
+    acc += x * x;
+  }
+  return acc;
 }
 
 __global__ __launch_bounds__(256) void grad_sumsq_kernel(GradTable t, double* __restrict__ partial) {
-  __shared__ double red[256];
+  __shared__ double red[4];
+  const TensorFinder find(t);
   double acc = 0.0;
   for (unsigned tile = blockIdx.x; tile < t.tiles; tile += gridDim.x) {
-    const GradEntry& e = t.e[find_tensor(t, tile)];
-    const size_t begin = (size_t)(tile - e.first) * kTile, end = begin + kTile < e.count ? begin + kTile : e.count;
-    for (size_t i = begin + threadIdx.x; i < end; i += 256) {
-      const double x = e.bf16 ? ld(static_cast<const bf16*>(e.in) + i) : ld(static_cast<const float*>(e.in) + i);
-      acc += x * x;
-    }
+    const GradEntry& e = t.e[find(tile)];
+    if (tile < kKeepTiles) acc += e.bf16 ? tile_sumsq<bf16, true>(e, tile) : tile_sumsq<float, true>(e, tile);
+    else acc += e.bf16 ? tile_sumsq<bf16, false>(e, tile) : tile_sumsq<float, false>(e, tile);
   }
-  acc = block_sum(acc, red);
+  acc = sum_256(acc, red);
   if (threadIdx.x == 0) partial[blockIdx.x] = acc;
 }
 
 __global__ __launch_bounds__(256) void grad_finish_kernel(const double* __restrict__ partial, size_t n, double* __restrict__ sumsq) {
-  __shared__ double red[256];
+  __shared__ double red[4];
   double acc = 0.0;
+#pragma unroll 8
   for (size_t i = threadIdx.x; i < n; i += 256) acc += partial[i];
-  acc = block_sum(acc, red);
+  acc = sum_256(acc, red);
   if (threadIdx.x == 0) sumsq[0] = acc;
 }
 
+template <typename T>
+__device__ __forceinline__ void tile_scale(const GradEntry& e, unsigned tile, float scale) {
+  using Vec = typename std::conditional<sizeof(T) == 2, bf16x8, f32x4>::type;
+  const TileSplit<T> s(e, tile);
+  const T* in = static_cast<const T*>(e.in) + s.begin;
+  T* out = static_cast<T*>(e.out) + s.begin;
+  if ((reinterpret_cast<uintptr_t>(e.in) ^ reinterpret_cast<uintptr_t>(e.out)) & 15u) {  // no boundary in common
+    for (unsigned i = threadIdx.x; i < s.n; i += 256) st(out + i, ld(in + i) * scale);
+    return;
+  }
+  Vec v[kLoads];
+  if (s.vecs) {
+#pragma unroll
+    for (int u = 0; u < kLoads; ++u)
+      v[u] = fetch<true>(reinterpret_cast<const Vec*>(in + s.head + min(threadIdx.x + 256u * u, s.vecs - 1) * s.kVec));
+  }
+#pragma unroll
+  for (int u = 0; u < kLoads; ++u) {
+    const unsigned at = threadIdx.x + 256u * u;
+    if (at >= s.vecs) break;
+    Vec o;
+#pragma unroll
+    for (unsigned j = 0; j < s.kVec; ++j) o[j] = (T)((float)v[u][j] * scale);
+    put<true>(reinterpret_cast<Vec*>(out + s.head + at * s.kVec), o);
+  }
+  const unsigned i = s.loose(threadIdx.x);
+  if (i < s.n) st(out + i, ld(in + i) * scale);
+}
+
 __global__ __launch_bounds__(256) void grad_clip_kernel(GradTable t, ClipArgs c) {
+  const TensorFinder find(t);
   const ClipScale s = clip_scale(c);
   if (c.norm && blockIdx.x == 0 && threadIdx.x == 0) c.norm[0] = s.norm;
   for (unsigned tile = blockIdx.x; tile < t.tiles; tile += gridDim.x) {
-    const GradEntry& e = t.e[find_tensor(t, tile)];
+    const GradEntry& e = t.e[find(tile)];
     if (s.scale == 1.f && e.in == e.out) continue;
-    const size_t begin = (size_t)(tile - e.first) * kTile, end = begin + kTile < e.count ? begin + kTile : e.count;
-    for (size_t i = begin + threadIdx.x; i < end; i += 256) {
-      if (e.bf16) st(static_cast<bf16*>(e.out) + i, ld(static_cast<const bf16*>(e.in) + i) * s.scale);
-      else st(static_cast<float*>(e.out) + i, ld(static_cast<const float*>(e.in) + i) * s.scale);
-    }
+    if (e.bf16) tile_scale<bf16>(e, tile, s.scale);
+    else tile_scale<float>(e, tile, s.scale);
   }
 }
 
@@ -104,7 +191,8 @@ size_t fill_table(const hanayo_grad* grads, size_t n, size_t at, GradTable& t) {
     ++taken;
     if (!g.count) continue;
     t.e[t.n++] = GradEntry{g.grad, g.out ? g.out : const_cast<void*>(g.grad), g.count, t.tiles, g.dtype == HANAYO_BF16};
-    t.tiles += (unsigned)((g.count + kTile - 1) / kTile);  // at most 2^40 elements together (kGradMaxElements): 2^27 tiles
+    const size_t each = kTileBytes / (g.dtype == HANAYO_BF16 ? 2 : 4);
+    t.tiles += (unsigned)((g.count + each - 1) / each);  // at most 2^40 elements together (kGradMaxElements): 2^27 tiles
   }
   return taken;
 }
