@@ -46,6 +46,26 @@ __device__ __forceinline__ void store8(bf16* p, const float (&v)[8]) {
   *reinterpret_cast<bf16x8*>(p) = a;
 }
 
+// Eight consecutive elements in storage form: what a load that is still in flight occupies (for bf16 a
+// quarter of the registers of eight floats).
+template <typename T>
+struct Raw8;
+template <>
+struct Raw8<bf16> {
+  bf16x8 v;
+  __device__ __forceinline__ void load(const bf16* p) { v = *reinterpret_cast<const bf16x8*>(p); }
+  __device__ __forceinline__ float get(int j) const { return (float)v[j]; }
+};
+template <>
+struct Raw8<float> {
+  f32x4 v[2];
+  __device__ __forceinline__ void load(const float* p) {
+    v[0] = *reinterpret_cast<const f32x4*>(p);
+    v[1] = *reinterpret_cast<const f32x4*>(p + 4);
+  }
+  __device__ __forceinline__ float get(int j) const { return v[j >> 2][j & 3]; }
+};
+
 __device__ __forceinline__ float ld(const float* p) { return *p; }
 __device__ __forceinline__ float ld(const bf16* p) { return (float)*p; }
 __device__ __forceinline__ void st(float* p, float v) { *p = v; }

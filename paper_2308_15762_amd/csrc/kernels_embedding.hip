@@ -35,6 +35,9 @@ __global__ __launch_bounds__(256) void embedding_fwd_kernel(const T* __restrict_
   }
 }
 
+typedef __attribute__((ext_vector_type(4))) int i32x4;
+typedef __attribute__((ext_vector_type(4), aligned(4))) int i32x4_any;  // four tokens, on any token's boundary
+
 // ------------------------------------------------------------------ rows sorted by token
 // Keys are tokens; one outside [0, vocab) counts as `vocab` and goes to the end.  Two ways to the same order:
 // few rows: every row counts the rows before it (one launch); many rows: radix sort (two launches for every 9 bits of the vocabulary).
@@ -42,46 +45,70 @@ __device__ __forceinline__ int token_key(const int32_t* tokens, int t, int vocab
 
 // The table's gradient is cleared by workgroups of the first launch, beside those that sort.
 __device__ __forceinline__ void clear_share(f32x4* out, size_t n, int share, int shares, int threads) {
-  for (size_t i = (size_t)share * threads + threadIdx.x; i < n; i += (size_t)shares * threads) out[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+  const size_t step = (size_t)shares * threads;
+#pragma unroll 4
+  for (size_t i = (size_t)share * threads + threadIdx.x; i < n; i += step) 
+    put<true>(out + i, f32x4{0.f, 0.f, 0.f, 0.f});
 }
 
-// Where each row goes: the number of rows that sort before it, by token and, among equal tokens, by row.  A workgroup places 64
-// rows, a row per lane; its 16 wavefronts compare them with a sixteenth of all rows each, whose tokens are uniform over the
-// wavefront and come through scalar loads.
+// Where each row goes: the number of rows that sort before it, by token and, among equal tokens, by row.  A workgroup places 16
+// rows: a lane compares row lane % 16 with four tokens of every sixteen that its wavefront takes from LDS, so that the comparisons
+// spread over four times the CUs that a row per lane would use.  Tokens before the 16 rows count where they are at most the row's,
+// tokens behind them where they are less.
 __global__ __launch_bounds__(1024) void token_rank_kernel(const int32_t* __restrict__ tokens, int rows, int vocab,
                                                           int32_t* __restrict__ order, int32_t* __restrict__ sorted, int sorters,
                                                           f32x4* __restrict__ clear, size_t clear_n) {
-  __shared__ int part[16][64];
+  __shared__ int part[16][16];
+  extern __shared__ i32x4 keys[];  // all rows' keys, behind the last row ones that sort behind everything
   if ((int)blockIdx.x >= sorters) {
     clear_share(clear, clear_n, blockIdx.x - sorters, gridDim.x - sorters, 1024);
     return;
   }
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int first = blockIdx.x * 64, t = first + lane;
-  const int mine = t < rows ? token_key(tokens, t, vocab) : 0;
-  const int each = (rows + 15) / 16, begin = wave * each, end = min(begin + each, rows);
-  int before = 0;
-#pragma unroll 16
-  for (int s = begin; s < min(end, first); ++s) before += token_key(tokens, s, vocab) <= mine;
-  for (int s = max(begin, first); s < min(end, first + 64); ++s) {
-    const int other = token_key(tokens, s, vocab);
-    before += other < mine || (other == mine && s < t);
+  const int own = blockIdx.x, t = own * 16 + (lane & 15), quad = lane >> 4;
+  const int spans = (rows + 15) / 16;
+  for (int q = threadIdx.x; q < spans * 4; q += 1024) {
+    i32x4 v;
+    if (q * 4 + 4 <= rows) {
+      v = *reinterpret_cast<const i32x4_any*>(tokens + q * 4);
+    } else {
+#pragma unroll
+      for (int k = 0; k < 4; ++k) v[k] = q * 4 + k < rows ? tokens[q * 4 + k] : -1;
+    }
+#pragma unroll
+    for (int k = 0; k < 4; ++k) v[k] = q * 4 + k < rows ? (int)min((unsigned)v[k], (unsigned)vocab) : -1;
+    keys[q] = v;
   }
-#pragma unroll 16
-  for (int s = max(begin, first + 64); s < end; ++s) before += token_key(tokens, s, vocab) < mine;
-  part[wave][lane] = before;
   __syncthreads();
-  if (wave == 0 && t < rows) {
+  const unsigned mine = (unsigned)reinterpret_cast<const int*>(keys)[t];
+  int before = 0;
+#pragma unroll 8
+  for (int span = wave; span < spans; span += 16) {
+    const i32x4 v = keys[span * 4 + quad];
+    const unsigned below = span < own ? mine + 1 : mine;  // mine is at most 2^31 - 1 where it counts
+#pragma unroll
+    for (int k = 0; k < 4; ++k) before += (unsigned)v[k] < below;
+  }
+  if (wave == own % 16) {
+    const i32x4 v = keys[own * 4 + quad];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) before += (unsigned)v[k] == mine && quad * 4 + k < (lane & 15);
+  }
+  before += __shfl_xor(before, 16);
+  before += __shfl_xor(before, 32);
+  if (lane < 16) part[wave][lane] = before;
+  __syncthreads();
+  if (threadIdx.x < 16 && t < rows) {
     int at = 0;
 #pragma unroll
     for (int w = 0; w < 16; ++w) at += part[w][lane];
     order[at] = t;
-    sorted[at] = mine;
+    sorted[at] = (int)mine;
   }
 }
 
 // Radix sort by one digit: workgroup b owns the b-th run of `each` keys.  `counts` [workgroups][bins]: how often each digit occurs in each run.
-constexpr int kMaxBins = 512, kMaxSorters = 256, kSortWaves = 4;
+constexpr int kMaxBins = 512, kMaxSorters = 256, kSortWaves = 16;
 struct SortArgs {
   const int32_t* tokens;  // the first pass: keys from the tokens, rows in order; later passes: nullptr
   const int32_t *order_in, *sorted_in;
@@ -105,53 +132,65 @@ __global__ __launch_bounds__(256) void sort_count_kernel(SortArgs a, f32x4* __re
 }
 
 // Moves a run's keys to their places: behind the keys of smaller digits and those of the same digit in earlier runs and earlier
-// wavefronts (a wavefront owns a quarter of the run), in order.  64 keys at a time: a ballot for each bit of the digit finds the
-// lanes with the same one.
-__global__ __launch_bounds__(kSortWaves * 64) void sort_place_kernel(SortArgs a) {
+// wavefronts (a wavefront owns a sixteenth of the run), in order.  64 keys at a time: a ballot for each bit of the digit finds the
+// lanes with the same one.  The counts of all runs are read by all 1024 threads: two digits each, every fourth run.
+__global__ __launch_bounds__(kSortWaves * 64) void sort_place_kernel(SortArgs a, f32x4* __restrict__ clear, size_t clear_n) {
   __shared__ int at[kSortWaves][kMaxBins];  // where the wavefront's next key of a digit goes
-  __shared__ int scan[kSortWaves * 64];
+  __shared__ int2 sums[2][4][kMaxBins / 2];  // of each group of runs: keys of a digit in all runs, in earlier runs
+  __shared__ int wave_total[kSortWaves];
+  if ((int)blockIdx.x >= a.sorters) {
+    clear_share(clear, clear_n, blockIdx.x - a.sorters, gridDim.x - a.sorters, kSortWaves * 64);
+    return;
+  }
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, bins = 1 << a.bits;
   const int begin = blockIdx.x * a.each, end = min(begin + a.each, a.rows);
-  const int quarter = (a.each / kSortWaves), w0 = min(begin + wave * quarter, end), w1 = min(w0 + quarter, end);
-  for (int d = threadIdx.x; d < kSortWaves * kMaxBins; d += 256) at[d / kMaxBins][d % kMaxBins] = 0;
-  __syncthreads();
+  const int share = a.each / kSortWaves, w0 = min(begin + wave * share, end), w1 = min(w0 + share, end);
+  for (int d = lane; d < bins; d += 64) at[wave][d] = 0;  // its own counters: no other wavefront sees them yet
   for (int i = w0 + lane; i < w1; i += 64) atomicAdd(&at[wave][sort_key(a, i) >> a.shift & (bins - 1)], 1);
-  // a thread owns two neighbouring digits: their totals, and their counts in earlier runs
-  const int d0 = threadIdx.x * 2;
-  int total[2] = {0, 0}, earlier[2] = {0, 0};
-  if (d0 < bins) {
+  const int pair = threadIdx.x % (kMaxBins / 2), group = threadIdx.x / (kMaxBins / 2);
+  int2 total = make_int2(0, 0), earlier = make_int2(0, 0);
+  if (2 * pair < bins) {
 #pragma unroll 16
-    for (int b = 0; b < a.sorters; ++b) {
-      const int2 c = *reinterpret_cast<const int2*>(a.counts + b * bins + d0);
-      total[0] += c.x;
-      total[1] += c.y;
-      if (b < (int)blockIdx.x) {
-        earlier[0] += c.x;
-        earlier[1] += c.y;
-      }
+    for (int b = group; b < a.sorters; b += 4) {
+      const int2 c = *reinterpret_cast<const int2*>(a.counts + b * bins + 2 * pair);
+      const int mine = b < (int)blockIdx.x ? -1 : 0;
+      total.x += c.x;
+      total.y += c.y;
+      earlier.x += c.x & mine;
+      earlier.y += c.y & mine;
     }
   }
-  int sum = total[0] + total[1];
-  scan[threadIdx.x] = sum;
+  sums[0][group][pair] = total;
+  sums[1][group][pair] = earlier;
   __syncthreads();
-  for (int o = 1; o < kSortWaves * 64; o <<= 1) {
-    const int add = (int)threadIdx.x >= o ? scan[threadIdx.x - o] : 0;
-    __syncthreads();
-    scan[threadIdx.x] += add;
-    __syncthreads();
+  // a thread per digit: the keys of smaller digits (a running sum over the lanes and the wavefronts before), then the places of the
+  // digit's keys in this run, wavefront by wavefront
+  const int d = threadIdx.x;
+  const int* all = reinterpret_cast<const int*>(sums);
+  int n = 0, ahead = 0;
+  if (d < bins) {
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      n += all[g * kMaxBins + d];
+      ahead += all[(4 + g) * kMaxBins + d];
+    }
   }
-  if (d0 < bins) {
-    int base = scan[threadIdx.x] - sum;
+  int upto = n;
 #pragma unroll
-    for (int k = 0; k < 2; ++k) {
-      int next = base + earlier[k];
+  for (int o = 1; o < 64; o <<= 1) {
+    const int add = __shfl_up(upto, o);
+    if (lane >= o) upto += add;
+  }
+  if (lane == 63) wave_total[wave] = upto;
+  __syncthreads();
+  if (d < bins) {
+    int next = upto - n + ahead;
+    for (int w = 0; w < wave; ++w) next += wave_total[w];
 #pragma unroll
-      for (int w = 0; w < kSortWaves; ++w) {
-        const int n = at[w][d0 + k];
-        at[w][d0 + k] = next;
-        next += n;
-      }
-      base += total[k];
+    for (int w = 0; w < kSortWaves; ++w) {
+      const int c = at[w][d];
+      at[w][d] = next;
+      next += c;
     }
   }
   __syncthreads();
@@ -167,7 +206,7 @@ __global__ __launch_bounds__(kSortWaves * 64) void sort_place_kernel(SortArgs a)
     }
     const int before = __popcll(same & ((1ull << lane) - 1ull));
     if (have) {
-      const int to = at[wave][digit] + before;  // the wavefront's own counters, read before the first of the lanes moves them on
+      const int to = at[wave][digit] + before;  // read by all lanes before the first of them moves the counter on
       a.order_out[to] = a.tokens ? i : a.order_in[i];
       a.sorted_out[to] = key;
     }
@@ -180,107 +219,269 @@ __global__ __launch_bounds__(kSortWaves * 64) void sort_place_kernel(SortArgs a)
 }
 
 // ------------------------------------------------------------------ sums over the runs of equal tokens
-// The sorted rows are cut into pieces of `R` (16 .. 64), a wavefront per piece and 512 columns, so that the work is even whatever the tokens: a token's
-// run that lies within a piece is added up and written; of one that crosses a border the piece leaves its part as a partial sum (slot 0: the
-// run comes from the piece before; slot 1: it starts here), and the kernel below adds those.  The piece's tokens and rows lie in
-// the lanes; eight rows, and the old sums of the runs that end among them, are loaded at a time.
+// The sorted rows are cut into pieces of R (8 .. 64), a wavefront per piece and 512 columns, so that the work is even whatever the
+// tokens: a run of a token that lies within a piece is added up and written; of one that crosses a border the piece leaves its part
+// in LDS (slot 0: the run comes from the piece before; slot 1: it starts here).  The workgroup then goes through its eight pieces'
+// parts in order: runs that lie within the workgroup's rows are written, and of those that cross its border it leaves its part in
+// memory, in two slots again, which the kernel below adds up.  A piece's tokens and rows lie in the lanes; eight rows are loaded
+// while the eight before them are added.
+constexpr int kPieces = 8;  // of a workgroup
 template <typename T, bool ADD>
-__global__ __launch_bounds__(256) void embedding_sum_kernel(const int32_t* __restrict__ order, const int32_t* __restrict__ sorted,
-                                                            const T* __restrict__ dout, float scale, float* __restrict__ d_table,
-                                                            float* __restrict__ partial, int rows, int H, int vocab, int R) {
+__global__ __launch_bounds__(kPieces * 64) void embedding_sum_kernel(const int32_t* __restrict__ order, const int32_t* __restrict__ sorted,
+                                                                     const T* __restrict__ dout, float scale,
+                                                                     float* __restrict__ d_table, float* __restrict__ partial, int rows,
+                                                                     int H, int vocab, int R, int slabs) {
+  __shared__ float parts[kPieces][2][512];
+  __shared__ int left[kPieces];  // what a piece left: bit 0 slot 0, bit 1 slot 1, bit 2: the run of slot 0 ends in the piece
+  __shared__ int run_of[kPieces];  // the token of the piece's first row, that of slot 0
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int piece = blockIdx.x * 4 + wave, c = (blockIdx.y * 64 + lane) * 8;
-  const long p0 = (long)piece * R;
-  if (p0 >= rows) return;
-  const int n = min(R, (int)(rows - p0));
-  const int tok = lane < n ? sorted[p0 + lane] : -1, row = lane < n ? order[p0 + lane] : 0;
-  const int before = p0 > 0 ? sorted[p0 - 1] : -1, after = p0 + n < rows ? sorted[p0 + n] : -1;
-  const int live = __popcll(__ballot(lane < n && tok < vocab));
-  if (live == 0) return;
-  const int next = __shfl_down(tok, 1);
-  const unsigned long long ends = __ballot(lane < n && (lane == n - 1 || tok != next));  // the last rows of runs
-  unsigned long long whole = ends;                                                       // of runs that lie in the piece
-  bool head = before == __builtin_amdgcn_readfirstlane(tok);                             // the first run comes from before
-  if (head) whole &= whole - 1;
-  if (after == __builtin_amdgcn_readlane(tok, n - 1)) whole &= ~(1ull << (n - 1));
+  // the slabs of a group of pieces follow each other, so that their rows are read at one time
+  const int group = blockIdx.x / slabs, slab = blockIdx.x - group * slabs;
+  const int c = (slab * 64 + lane) * 8;
   const bool inside = c < H;
-  float acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-  constexpr int U = 8;
-  for (int i0 = 0; i0 < live; i0 += U) {
-    float v[U][8], old[U][8];
-    if (inside) {
+  const long p0 = ((long)group * kPieces + wave) * R;
+  const int n = p0 < rows ? min(R, (int)(rows - p0)) : 0;
+  const int tok = lane < n ? sorted[p0 + lane] : -1, row = lane < n ? order[p0 + lane] : 0;
+  const int before = p0 > 0 && n ? sorted[p0 - 1] : -1, after = p0 + n < rows ? sorted[p0 + n] : -1;
+  const int live = __popcll(__ballot(lane < n && tok < vocab));
+  if (lane == 0) left[wave] = 0;
+  if (live) {
+    const int first = __builtin_amdgcn_readfirstlane(tok);
+    const int next = __shfl_down(tok, 1);
+    const unsigned long long ends = __ballot(lane < n && (lane == n - 1 || tok != next));  // the last rows of runs
+    unsigned long long whole = ends;                                                       // of runs that lie in the piece
+    bool head = before == first;                                                           // the first run comes from before
+    const bool tail = after == __builtin_amdgcn_readlane(tok, n - 1);                      // the last one goes on
+    if (lane == 0) {
+      const bool one = (ends & (ends - 1)) == 0;  // a single run
+      left[wave] = (head ? 1 | (one && tail ? 0 : 4) : 0) | (tail && !(one && head) ? 2 : 0);
+      run_of[wave] = first;
+    }
+    if (head) whole &= whole - 1;
+    if (tail) whole &= ~(1ull << (n - 1));
+    float acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    constexpr int U = sizeof(T) == 2 ? 8 : 4;
+    Raw8<T> rows_now[U], rows_next[U];
+    auto fetch_rows = [&](Raw8<T>(&v)[U], int i0) {
 #pragma unroll
-      for (int u = 0; u < U; ++u)
-        load8(dout + (size_t)__builtin_amdgcn_readlane(row, min(i0 + u, live - 1)) * H + c, v[u]);
-      if constexpr (ADD) {
+      for (int u = 0; u < U; ++u) v[u].load(dout + (size_t)__builtin_amdgcn_readlane(row, min(i0 + u, live - 1)) * H + c);
+    };
+    if (inside) fetch_rows(rows_next, 0);
+    for (int i0 = 0; i0 < live; i0 += U) {
+      float old[U][8];
+      if (inside) {
+        if constexpr (ADD) {
 #pragma unroll
-        for (int u = 0; u < U; ++u)
-          if (i0 + u < live && (whole >> (i0 + u) & 1))
-            load8(d_table + (size_t)__builtin_amdgcn_readlane(tok, i0 + u) * H + c, old[u]);
+          for (int u = 0; u < U; ++u)
+            if (i0 + u < live && (whole >> (i0 + u) & 1))
+              load8(d_table + (size_t)__builtin_amdgcn_readlane(tok, i0 + u) * H + c, old[u]);
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) rows_now[u] = rows_next[u];
+        if (i0 + U < live) fetch_rows(rows_next, i0 + U);
       }
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int i = i0 + u;
+        if (i >= live) break;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) acc[j] += rows_now[u].get(j);
+        if (ends >> i & 1) {
+          if (whole >> i & 1) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) acc[j] = ADD ? old[u][j] + scale * acc[j] : scale * acc[j];
+            if (inside) store8(d_table + (size_t)__builtin_amdgcn_readlane(tok, i) * H + c, acc);
+          } else {
+            store8(&parts[wave][head ? 0 : 1][lane * 8], acc);
+          }
+          head = false;
+#pragma unroll
+          for (int j = 0; j < 8; ++j) acc[j] = 0.f;
+        }
+      }
+    }
+  }
+  __syncthreads();
+  // a thread per column
+  const int col = threadIdx.x, gc = slab * 512 + col;
+  static_assert(kPieces * 64 == 512, "a thread per column");
+  if (gc >= H) return;
+  float* mine = partial + (size_t)group * 2 * H + gc;
+  float run = 0.f;
+  bool open = false, ours = false;  // a run goes on; it starts in these pieces
+  for (int w = 0; w < kPieces; ++w) {
+    const int what = left[w];
+    if (what & 1) {
+      run = open ? run + parts[w][0][col] : parts[w][0][col];
+      open = true;
+      if (what & 4) {
+        if (ours) {
+          float* dst = d_table + (size_t)run_of[w] * H + gc;
+          *dst = ADD ? *dst + scale * run : scale * run;
+        } else {
+          mine[0] = run;
+        }
+        open = ours = false;
+      }
+    }
+    if (what & 2) {
+      run = parts[w][1][col];
+      open = ours = true;
+    }
+  }
+  if (open) mine[ours ? H : 0] = run;
+}
+
+// The runs that cross a border between workgroups of the kernel above (`R` rows each here), each by the wavefront of the piece that it starts in: that piece's slot
+// 1 and slot 0 of the pieces behind it.  Runs over many pieces are listed and then added by all wavefronts of the workgroup, every eighth partial sum
+// each, whose sums are added in order.
+constexpr int kJoinWaves = 8, kJoinAlone = 16;
+struct JoinArgs {
+  const int32_t* sorted;
+  const float* partial;
+  float scale;
+  float* d_table;
+  int rows, H, vocab, R;
+};
+__device__ __forceinline__ void join_partials(const JoinArgs& a, int piece, int first, int n, int step, int c, float (&acc)[8]) {
+#pragma unroll
+  for (int j = 0; j < 8; ++j) acc[j] = 0.f;
+  constexpr int U = 16;  // loads in flight; behind the last one it is read again and not added
+  for (int k0 = first; k0 < n; k0 += U * step) {
+    float v[U][8];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int k = min(k0 + u * step, n - 1);
+      load8(a.partial + ((size_t)(piece + k) * 2 + (k == 0 ? 1 : 0)) * a.H + c, v[u]);
     }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const int i = i0 + u;
-      if (i >= live) break;
+      if (k0 + u * step >= n) break;
 #pragma unroll
       for (int j = 0; j < 8; ++j) acc[j] += v[u][j];
-      if (ends >> i & 1) {
-        if (whole >> i & 1) {
-#pragma unroll
-          for (int j = 0; j < 8; ++j) acc[j] = ADD ? old[u][j] + scale * acc[j] : scale * acc[j];
-          if (inside) store8(d_table + (size_t)__builtin_amdgcn_readlane(tok, i) * H + c, acc);
-        } else if (inside) {
-          store8(partial + ((size_t)piece * 2 + (head ? 0 : 1)) * H + c, acc);
-        }
-        head = false;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) acc[j] = 0.f;
-      }
     }
   }
 }
-
-// The runs that cross a piece's end, each by the workgroup of the piece that it starts in: that piece's slot 1 and slot 0 of
-// the pieces behind it, every kJoinWaves-th by one wavefront, and the wavefronts' sums in order.
-constexpr int kJoinWaves = 8;
 template <bool ADD>
-__global__ __launch_bounds__(kJoinWaves * 64) void embedding_join_kernel(const int32_t* __restrict__ sorted, const float* __restrict__ partial,
-                                                                         float scale, float* __restrict__ d_table, int rows, int H,
-                                                                         int vocab, int R) {
+__device__ __forceinline__ void join_store(const JoinArgs& a, int tok, int c, float (&acc)[8]) {
+  float* dst = a.d_table + (size_t)tok * a.H + c;
+  float old[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+  if constexpr (ADD) load8(dst, old);
+#pragma unroll
+  for (int j = 0; j < 8; ++j) old[j] += a.scale * acc[j];
+  store8(dst, old);
+}
+template <bool ADD>
+__global__ __launch_bounds__(kJoinWaves * 64) void embedding_join_kernel(JoinArgs a) {
   __shared__ float part[kJoinWaves][512];
+  __shared__ int runs[kJoinWaves][3];  // piece, token, partial sums (0: nothing for the workgroup)
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int piece = blockIdx.x, col = lane * 8, c = blockIdx.y * 512 + col;
-  const long p0 = (long)piece * R, p1 = p0 + R;
-  if (p1 >= rows) return;
-  const int tok = sorted[p1 - 1];
-  if (tok >= vocab || sorted[p1] != tok || (p0 > 0 && sorted[p0] == tok && sorted[p0 - 1] == tok)) return;
-  int n = 1;  // partial sums of the run
-  for (;; n += 64) {
-    const long q = (long)(piece + n + lane) * R;
-    const unsigned long long in = __ballot(q < rows && sorted[min(q, (long)rows - 1)] == tok);
-    if (in != ~0ull) {
-      n += __popcll(in);  // pieces of a run follow each other: the set bits are the lowest
-      break;
+  const int piece = blockIdx.x * kJoinWaves + wave, c = (blockIdx.y * 64 + lane) * 8;
+  const long p0 = (long)piece * a.R, p1 = p0 + a.R;
+  int n = 0, tok = 0;
+  if (p1 < a.rows) {
+    tok = a.sorted[p1 - 1];
+    if (tok < a.vocab && a.sorted[p1] == tok && !(p0 > 0 && a.sorted[p0] == tok && a.sorted[p0 - 1] == tok)) {
+      // pieces of a run follow each other: among 256 looked at together, those that hold the token are the first
+      for (n = 1;; n += 256) {
+        int in = 0;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const long q = (long)(piece + n + 64 * k + lane) * a.R;
+          in += __popcll(__ballot(q < a.rows && a.sorted[min(q, (long)a.rows - 1)] == tok));
+        }
+        if (in < 256) {
+          n += in;
+          break;
+        }
+      }
     }
   }
+  if (lane == 0) {
+    runs[wave][0] = piece;
+    runs[wave][1] = tok;
+    runs[wave][2] = n > kJoinAlone ? n : 0;
+  }
+  float acc[8];
+  if (n > 0 && n <= kJoinAlone && c < a.H) {
+    join_partials(a, piece, 0, n, 1, c, acc);
+    join_store<ADD>(a, tok, c, acc);
+  }
+  __syncthreads();
+  for (int r = 0; r < kJoinWaves; ++r) {
+    const int many = runs[r][2];  // the same for the whole workgroup
+    if (!many) continue;
+    if (c < a.H) join_partials(a, runs[r][0], wave, many, kJoinWaves, c, acc);
+    store8(part[wave] + lane * 8, acc);
+    __syncthreads();
+    if (wave == 0 && c < a.H) {
+      for (int w = 1; w < kJoinWaves; ++w) {
+        float v[8];
+        load8(part[w] + lane * 8, v);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) acc[j] += v[j];
+      }
+      join_store<ADD>(a, runs[r][1], c, acc);
+    }
+    __syncthreads();
+  }
+}
+
+// Few rows and a small table: a workgroup per token and 512 columns lists the token's rows, in order, and adds them up, every
+// fourth row by one wavefront; no sort, no second launch, and tokens that do not occur are cleared on the way.  512 columns: 128 rows
+// of 512 to 4096 tokens 6.8 us against 12.7 with the sort, 8192 tokens 7.6, 16384 tokens 12.2 against 13.4; 1024 rows of 4096 tokens
+// 8.9 against 14.1, 8192 tokens 13.1 against 15.0, 16384 tokens 23.2 against 17.0.
+constexpr int kDirectRows = 1024, kDirectGroups = 8192;
+template <typename T, bool ADD>
+__global__ __launch_bounds__(256) void embedding_direct_kernel(const int32_t* __restrict__ tokens, const T* __restrict__ dout,
+                                                               float scale, float* __restrict__ d_table, int rows, int H) {
+  __shared__ int list[kDirectRows];
+  __shared__ int counts[kDirectRows / 64];
+  __shared__ float part[4][512];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, tok = blockIdx.x, c = (blockIdx.y * 64 + lane) * 8;
+  const int groups = (rows + 63) / 64;
+  bool hit[kDirectRows / 256];
+  unsigned long long mask[kDirectRows / 256];
+#pragma unroll
+  for (int k = 0; k < kDirectRows / 256; ++k) {
+    const int t = k * 256 + threadIdx.x;
+    hit[k] = t < rows && tokens[t] == tok;
+    mask[k] = __ballot(hit[k]);
+    if (lane == 0) counts[k * 4 + wave] = __popcll(mask[k]);
+  }
+  __syncthreads();
+  int n = 0;
+#pragma unroll
+  for (int g = 0; g < kDirectRows / 64; ++g) {
+    if (g >= groups) break;
+    if ((g & 3) == wave && hit[g >> 2]) list[n + __popcll(mask[g >> 2] & ((1ull << lane) - 1ull))] = g * 64 + lane;
+    n += counts[g];
+  }
+  if (ADD && n == 0) return;
+  __syncthreads();
   float acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
   if (c < H) {
-#pragma unroll 8
-    for (int k = wave; k < n; k += kJoinWaves) {
-      float v[8];
-      load8(partial + ((size_t)(piece + k) * 2 + (k == 0 ? 1 : 0)) * H + c, v);
+    constexpr int U = 8;
+    for (int i0 = wave; i0 < n; i0 += 4 * U) {
+      Raw8<T> v[U];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) acc[j] += v[j];
+      for (int u = 0; u < U; ++u) v[u].load(dout + (size_t)list[min(i0 + 4 * u, n - 1)] * H + c);
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        if (i0 + 4 * u >= n) break;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) acc[j] += v[u].get(j);
+      }
     }
   }
-  store8(part[wave] + col, acc);
-  __syncthreads();
+  if (n > 1) {
+    store8(part[wave] + lane * 8, acc);
+    __syncthreads();
+  }
   if (wave || c >= H) return;
-  const int waves = min(n, kJoinWaves);
-  for (int w = 1; w < waves; ++w) {
+  for (int w = 1; w < min(n, 4); ++w) {
     float v[8];
-    load8(part[w] + col, v);
+    load8(part[w] + lane * 8, v);
 #pragma unroll
     for (int j = 0; j < 8; ++j) acc[j] += v[j];
   }
@@ -294,15 +495,27 @@ __global__ __launch_bounds__(kJoinWaves * 64) void embedding_join_kernel(const i
 
 __global__ __launch_bounds__(256) void clear_kernel(f32x4* __restrict__ out, size_t n) { clear_share(out, n, blockIdx.x, gridDim.x, 256); }
 
-// Up to so many rows the comparison of all pairs is the faster sort.
-constexpr int kRankRows = 16384;
+template <typename T>
+int embedding_direct(const int32_t* tokens, const void* dout, float scale, float* d_table, int rows, int H, int vocab, bool accumulate,
+                     hipStream_t stream) {
+  const dim3 grid(vocab, (H + 511) / 512);
+  if (accumulate)
+    launch_kernel((embedding_direct_kernel<T, true>), grid, dim3(256), 0, stream, tokens, (const T*)dout, scale, d_table, rows, H);
+  else
+    launch_kernel((embedding_direct_kernel<T, false>), grid, dim3(256), 0, stream, tokens, (const T*)dout, scale, d_table, rows, H);
+  return check_launch("embedding_backward (direct)");
+}
+// Up to so many rows the comparison of all pairs is the faster sort, and its keys fit the LDS (512 columns, whole call: 4096 rows
+// 15.5 us against 25.5 with the radix sort, 8192 rows 22.6 against 30.8, 12288 rows 30.0 against 32.1).
+constexpr int kRankRows = 12288;
 
-// Rows of a piece: enough pieces for four wavefronts on every SIMD where the rows allow it.
+// Rows of a piece: enough pieces for four wavefronts on every SIMD where the rows allow it (65521 rows of 1024, first of their
+// iteration: 16 rows 79 us, 32 rows 87, 8 rows 82; 4096 rows: 8 rows 17, 16 rows 20, 32 rows 27).
 int piece_rows(int rows, int H) {
   const long slabs = (H + 511) / 512;
-  for (int r = 64; r > 16; r /= 2)
+  for (int r = 64; r > 8; r /= 2)
     if ((long)rows / r * slabs >= 4096) return r;
-  return 16;
+  return 8;
 }
 
 struct EmbeddingLayout {
@@ -322,8 +535,8 @@ EmbeddingLayout embedding_layout(int rows, int H) {
     L.sorted[i] = take((size_t)rows * 4);
   }
   L.counts = take(radix ? (size_t)kMaxSorters * kMaxBins * 4 : 0);
-  const int r = piece_rows(rows, H);
-  L.partial = take(((size_t)rows + r - 1) / r * 2 * H * sizeof(float));
+  const int each = piece_rows(rows, H) * kPieces;
+  L.partial = take(((size_t)rows + each - 1) / each * 2 * H * sizeof(float));
   L.bytes = at;
   return L;
 }
@@ -331,13 +544,13 @@ EmbeddingLayout embedding_layout(int rows, int H) {
 template <typename T, bool ADD>
 int embedding_sums(const int32_t* order, const int32_t* sorted, const void* dout, float scale, float* d_table, float* partial, int rows,
                    int H, int vocab, hipStream_t stream) {
-  const int r = piece_rows(rows, H), pieces = (rows + r - 1) / r, slabs = (H + 511) / 512;
-  launch_kernel((embedding_sum_kernel<T, ADD>), dim3((pieces + 3) / 4, slabs), dim3(256), 0, stream, order, sorted, (const T*)dout, scale,
-                d_table, partial, rows, H, vocab, r);
+  const int r = piece_rows(rows, H), each = r * kPieces, groups = (rows + each - 1) / each, slabs = (H + 511) / 512;
+  launch_kernel((embedding_sum_kernel<T, ADD>), dim3((unsigned)((long)groups * slabs)), dim3(kPieces * 64), 0, stream, order, sorted,
+                (const T*)dout, scale, d_table, partial, rows, H, vocab, r, slabs);
   if (const int rc = check_launch("embedding_backward (sums)")) return rc;
-  if (pieces < 2) return HANAYO_OK;  // no border to cross
-  launch_kernel((embedding_join_kernel<ADD>), dim3(pieces - 1, slabs), dim3(kJoinWaves * 64), 0, stream, sorted, partial, scale, d_table,
-                rows, H, vocab, r);
+  if (groups < 2) return HANAYO_OK;  // no border to cross
+  launch_kernel((embedding_join_kernel<ADD>), dim3((groups - 1 + kJoinWaves - 1) / kJoinWaves, slabs), dim3(kJoinWaves * 64), 0, stream,
+                JoinArgs{sorted, partial, scale, d_table, rows, H, vocab, each});
   return check_launch("embedding_backward (join)");
 }
 
@@ -360,22 +573,25 @@ int embedding_backward(int dtype, const int32_t* tokens, const void* dout, float
                        bool accumulate, void* workspace, hipStream_t stream) {
   f32x4* clear = reinterpret_cast<f32x4*>(d_table);
   const size_t clear_n = accumulate ? 0 : (size_t)vocab * H / 4;
-  auto clearers = [&](int threads) {
-    const size_t want = (clear_n + threads - 1) / threads;
-    return (int)(want < 4096 ? want : 4096);
+  auto clearers = [&](size_t n, int threads) {
+    const size_t want = (n + threads - 1) / threads, most = (size_t)(1 << 20) / threads;
+    return (int)(want < most ? want : most);
   };
   if (rows == 0) {
     if (!clear_n) return HANAYO_OK;
-    launch_kernel(clear_kernel, dim3(clearers(256)), dim3(256), 0, stream, clear, clear_n);
+    launch_kernel(clear_kernel, dim3(clearers(clear_n, 256)), dim3(256), 0, stream, clear, clear_n);
     return check_launch("embedding_backward (clear)");
   }
+  if (rows <= kDirectRows && (long)vocab * ((H + 511) / 512) <= kDirectGroups)
+    return dtype == HANAYO_BF16 ? embedding_direct<bf16>(tokens, dout, scale, d_table, rows, H, vocab, accumulate, stream)
+                                : embedding_direct<float>(tokens, dout, scale, d_table, rows, H, vocab, accumulate, stream);
   char* ws = static_cast<char*>(workspace);
   const EmbeddingLayout L = embedding_layout(rows, H);
   auto ints = [&](size_t at) { return reinterpret_cast<int32_t*>(ws + at); };
   int32_t *order = ints(L.order[0]), *sorted = ints(L.sorted[0]);
   if (rows <= kRankRows) {
-    const int sorters = (rows + 63) / 64;
-    launch_kernel(token_rank_kernel, dim3(sorters + clearers(1024)), dim3(1024), 0, stream, tokens, rows, vocab, order, sorted, sorters,
+    const int sorters = (rows + 15) / 16;
+    launch_kernel(token_rank_kernel, dim3(sorters + clearers(clear_n, 1024)), dim3(1024), (size_t)sorters * 64, stream, tokens, rows, vocab, order, sorted, sorters,
                   clear, clear_n);
     if (const int rc = check_launch("embedding_backward (sort)")) return rc;
   } else {
@@ -388,15 +604,21 @@ int embedding_backward(int dtype, const int32_t* tokens, const void* dout, float
     a.each = ((rows + kMaxSorters - 1) / kMaxSorters + unit - 1) / unit * unit;
     if (a.each < 1024) a.each = 1024;
     a.sorters = (rows + a.each - 1) / a.each;
+    size_t cleared = 0;  // every launch of the sort, which keeps few CUs busy, clears its share of the table
     for (int pass = 0; pass < passes; ++pass) {
       a.shift = pass * bits / passes;
       a.bits = (pass + 1) * bits / passes - a.shift;
       const int to = pass & 1;
       a.order_out = ints(L.order[to]); a.sorted_out = ints(L.sorted[to]);
-      launch_kernel(sort_count_kernel, dim3(a.sorters + (pass ? 0 : clearers(256))), dim3(256), 0, stream, a, clear, clear_n);
-      if (const int rc = check_launch("embedding_backward (sort, count)")) return rc;
-      launch_kernel(sort_place_kernel, dim3(a.sorters), dim3(kSortWaves * 64), 0, stream, a);
-      if (const int rc = check_launch("embedding_backward (sort, place)")) return rc;
+      for (int step = 0; step < 2; ++step) {
+        const size_t upto = clear_n * (2 * pass + step + 1) / (2 * passes), n = upto - cleared;
+        if (step == 0)
+          launch_kernel(sort_count_kernel, dim3(a.sorters + clearers(n, 256)), dim3(256), 0, stream, a, clear + cleared, n);
+        else
+          launch_kernel(sort_place_kernel, dim3(a.sorters + clearers(n, kSortWaves * 64)), dim3(kSortWaves * 64), 0, stream, a, clear + cleared, n);
+        if (const int rc = check_launch("embedding_backward (sort)")) return rc;
+        cleared = upto;
+      }
       a.tokens = nullptr;
       a.order_in = a.order_out; a.sorted_in = a.sorted_out;
     }

@@ -19,26 +19,6 @@ namespace {
 constexpr int kRowsPerBlock = 4;  // wavefronts per 256-thread block
 constexpr int kLnBwdMaxBlocks = kLnPartialRows;  // workgroups of the LN backward = partial rows of gamma/beta sums it writes
 
-// Eight consecutive elements in storage form: what a load that is still in flight occupies (for bf16 a
-// quarter of the registers of eight floats).
-template <typename T>
-struct Raw8;
-template <>
-struct Raw8<bf16> {
-  bf16x8 v;
-  __device__ __forceinline__ void load(const bf16* p) { v = *reinterpret_cast<const bf16x8*>(p); }
-  __device__ __forceinline__ float get(int j) const { return (float)v[j]; }
-};
-template <>
-struct Raw8<float> {
-  f32x4 v[2];
-  __device__ __forceinline__ void load(const float* p) {
-    v[0] = *reinterpret_cast<const f32x4*>(p);
-    v[1] = *reinterpret_cast<const f32x4*>(p + 4);
-  }
-  __device__ __forceinline__ float get(int j) const { return v[j >> 2][j & 3]; }
-};
-
 // ------------------------------------------------------------------ LN forward
 // NV = vectors of 8 per lane kept in registers (H <= 64 * 8 * NV).  FULL: H == 512 * NV exactly, so no lane's
 // vector falls outside the row: the column guards vanish at compile time and a row's loads are one straight run
