@@ -225,6 +225,10 @@ def _ptr(t):
     return t.data_ptr()
 
 
+# the current device's index without torch.cuda.current_device()'s check that torch is initialised (a tensor is on the GPU, so it is)
+_current_device = torch._C._cuda_getDevice
+
+
 def _room(what, t, count, size):
     """Device address of an operand of `count` elements of `size` bytes: an integer address as it is, None as NULL; a tensor
     that is not on the current device, not contiguous, of another element size or too small is refused."""
@@ -235,7 +239,7 @@ def _room(what, t, count, size):
     if t.element_size() != size or t.numel() < count:
         raise HanayoError(EINVAL, "%s: %d elements of %d bytes are wanted, not %d of %d"
                           % (what, count, size, t.numel(), t.element_size()))
-    if t.get_device() != torch.cuda.current_device():
+    if t.get_device() != _current_device():
         raise HanayoError(EINVAL, "%s: the tensor is not on the current device" % what)
     return t.data_ptr()
 
