@@ -146,6 +146,8 @@ __global__ __launch_bounds__(kSortWaves * 64) void sort_place_kernel(SortArgs a,
   const int begin = blockIdx.x * a.each, end = min(begin + a.each, a.rows);
   const int share = a.each / kSortWaves, w0 = min(begin + wave * share, end), w1 = min(w0 + share, end);
   for (int d = lane; d < bins; d += 64) at[wave][d] = 0;  // its own counters: no other wavefront sees them yet
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
   for (int i = w0 + lane; i < w1; i += 64) atomicAdd(&at[wave][sort_key(a, i) >> a.shift & (bins - 1)], 1);
   const int pair = threadIdx.x % (kMaxBins / 2), group = threadIdx.x / (kMaxBins / 2);
   int2 total = make_int2(0, 0), earlier = make_int2(0, 0);

@@ -22,7 +22,7 @@ namespace {
 constexpr unsigned kTileBytes = 32768;  // of a tensor: eight 16-byte loads a thread, all in flight at once
 constexpr int kMaxBlocks = 2048;        // workgroups of a launch at most: 8 on every CU, one partial sum each
 constexpr int kLoads = kTileBytes / 16 / 256;
-// The pass that forms the norm leaves the first 192 MiB of a launch's tensors in the 256 MB cache and reads the rest past it, so that the pass
+// The pass that forms the norm leaves the first 192 MiB of a call's tensors in the 256 MB cache and reads the rest past it, so that the pass
 // that scales or uses them finds that part there; that pass reads and writes past the cache.  Norm and clipping of 403 MB:
 // 181 us, of 1013 us with Adam on 609 MB (30 bytes an element) 852; with ordinary loads and stores everywhere 238 and 1046, the rest past the
 // cache in the first pass only 200 and 1043, nothing kept 214 and 1013.
@@ -41,7 +41,7 @@ constexpr int kEntries = 100;  // 3.2 KB; kernel arguments end at 4 KB
 struct GradTable {
   GradEntry e[kEntries];
   int n;
-  unsigned tiles;
+  unsigned tiles, keep;  // keep: the first of them, that the norm's pass leaves in the cache
 };
 
 // Which tensor a tile lies in.  The lanes of a wavefront hold the tensors' first tiles, two each, and vote: one trip to memory
@@ -124,7 +124,7 @@ __global__ __launch_bounds__(256) void grad_sumsq_kernel(GradTable t, double* __
   double acc = 0.0;
   for (unsigned tile = blockIdx.x; tile < t.tiles; tile += gridDim.x) {
     const GradEntry& e = t.e[find(tile)];
-    if (tile < kKeepTiles) acc += e.bf16 ? tile_sumsq<bf16, true>(e, tile) : tile_sumsq<float, true>(e, tile);
+    if (tile < t.keep) acc += e.bf16 ? tile_sumsq<bf16, true>(e, tile) : tile_sumsq<float, true>(e, tile);
     else acc += e.bf16 ? tile_sumsq<bf16, false>(e, tile) : tile_sumsq<float, false>(e, tile);
   }
   acc = sum_256(acc, red);
@@ -184,7 +184,7 @@ __global__ __launch_bounds__(256) void grad_clip_kernel(GradTable t, ClipArgs c)
 // Fills the table with tensors from `at` on; returns how many it took.
 size_t fill_table(const hanayo_grad* grads, size_t n, size_t at, GradTable& t) {
   t.n = 0;
-  t.tiles = 0;
+  t.tiles = t.keep = 0;
   size_t taken = 0;
   while (at + taken < n && t.n < kEntries) {
     const hanayo_grad& g = grads[at + taken];
@@ -203,10 +203,13 @@ size_t grad_workspace_bytes(size_t n) { return ((n + kEntries - 1) / kEntries + 
 
 int grad_sumsq(const hanayo_grad* grads, size_t n, double* sumsq, double* workspace, hipStream_t stream) {
   size_t partials = 0;
+  unsigned keep = kKeepTiles;
   for (size_t at = 0; at < n;) {
     GradTable t;
     at += fill_table(grads, n, at, t);
     if (!t.tiles) continue;
+    t.keep = keep < t.tiles ? keep : t.tiles;
+    keep -= t.keep;
     const unsigned blocks = t.tiles < (unsigned)kMaxBlocks ? t.tiles : kMaxBlocks;
     launch_kernel(grad_sumsq_kernel, dim3(blocks), dim3(256), 0, stream, t, workspace + partials);
     if (const int rc = check_launch("grad_sumsq")) return rc;
