@@ -207,6 +207,7 @@ def main():
                     help="rank 0 also embeds the tokens in front of stage 0 and ends the last stage in head + loss "
                          "(not part of the headline metric's step; its flops are added to the TFLOP/s figure)")
     ap.add_argument("--adam", action="store_true", help="every step ends with the Adam update of all the rank's parameters")
+    ap.add_argument("--max-norm", type=float, default=None, help="with --adam: the gradients are clipped to this norm in the update")
     ap.add_argument("--copy-yardstick", type=int, nargs="*", metavar="MIB", default=None,
                     help="instead of the benchmark: time the plain copy kernel at these sizes (MiB read and as many "
                          "written; default 4 8 16 32 64 256), the yardstick of the memory-bound kernels")
@@ -242,7 +243,7 @@ def main():
             gpu.zero_grads()
         peak = gpu.run()
         if args.adam:
-            gpu.adam_step(1e-4, weight_decay=0.01)                            # clears the gradients as it goes
+            gpu.adam_step(1e-4, weight_decay=0.01, max_norm=args.max_norm)                            # clears the gradients as it goes
         return peak
 
     # one plain copy of known size: the dispatch the HBM traffic counters of a profiler run are scaled by
@@ -276,7 +277,7 @@ def main():
         "config": {"workload": "%s: rank %d of P=%d W=%d M=%d, %d tasks/step, chunk = %d %s-LN blocks H=%d heads=%d "
                                "F=%d seq=%d mb=%d" % (wl.name, rank, wl.P, wl.W, wl.M, n_tasks, wl.n_blocks, wl.norm,
                                                       wl.hidden, wl.heads, wl.ffn, wl.seq, wl.mb),
-                   "executor_lanes": args.lanes, "stash": args.stash, "model_ends": bool(args.ends), "adam": bool(args.adam), "stash_peak": peak, "stash_arena_gib": gpu.arena_bytes / 2 ** 30},
+                   "executor_lanes": args.lanes, "stash": args.stash, "model_ends": bool(args.ends), "adam": bool(args.adam), "max_norm": args.max_norm, "stash_peak": peak, "stash_arena_gib": gpu.arena_bytes / 2 ** 30},
         "roofline": {"bound": "mfma", "achieved": achieved, "peak": PEAK_BF16_TFLOPS, "unit": "TFLOP/s",
                      "frac": achieved / PEAK_BF16_TFLOPS, "traffic": stored_traffic(wl),
                      "kernel": "gemm_dma_kernel (bf16 MFMA; the %d GEMM launches of one block fwd+bwd, alone on the chip)" % n_gemm,

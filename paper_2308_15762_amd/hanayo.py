@@ -226,7 +226,7 @@ def _ptr(t):
 
 
 # the current device's index without torch.cuda.current_device()'s check that torch is initialised (a tensor is on the GPU, so it is)
-_current_device = torch._C._cuda_getDevice
+_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 
 
 def _room(what, t, count, size):

@@ -186,16 +186,36 @@ class GpuRank:
         self.opt = [dict(kind=k, w=w, g=g, master=w.float() if bf16 else None, m=torch.zeros_like(g),
                          v=torch.zeros_like(g)) for k, w, g in groups]
         self.opt_step = 0
+        self.grad_list = hn.grad_list([o["g"] for o in self.opt])
+        self.grad_work = dev_bytes(hn.hanayo_op_grad_workspace_bytes(len(self.opt)))
+        self.sumsq = torch.zeros(1, dtype=torch.float64, device="cuda")
+        self.grad_norm = torch.zeros(1, dtype=torch.float32, device="cuda")
 
-    def adam_step(self, lr, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.0, zero_grads=True, stream=None):
+    def grad_sumsq(self, stream=None):
+        """The squared norm of all gradients that the rank holds, a float64 tensor on the GPU: what ranks exchange before they clip."""
+        hn.hanayo_op_grad_sumsq(self.grad_list, self.sumsq, self.grad_work, stream)
+        return self.sumsq
+
+    def adam_step(self, lr, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.0, zero_grads=True, stream=None, max_norm=None,
+                  sumsq=None):
         """One update of everything the rank owns, to be called after run(): the flush of the iteration.
-        Decay goes to the chunks' matrices and the tables, not to biases and LayerNorm parameters."""
+        Decay goes to the chunks' matrices and the tables, not to biases and LayerNorm parameters.
+        max_norm: the gradients are scaled down to this norm on the way; grad_norm then holds the norm before.  sumsq: the
+        squared norms of all ranks (float64, on the GPU; default: of this rank alone).  A norm that is not finite leaves parameters
+        and moments as they are."""
         self.opt_step += 1
+        if max_norm is not None:
+            sumsq = self.grad_sumsq(stream) if sumsq is None else sumsq
+            clip = hn.make_clip(sumsq, sumsq.numel(), max_norm, self.grad_norm)
         dt = hn.BF16 if self.wl.dtype == "bf16" else hn.FP32
         for o in self.opt:
             wd = 0.0 if o["kind"] == "lnf" else weight_decay
             adam = hn.Adam(lr, beta1, beta2, eps, wd, self.opt_step, int(zero_grads))
-            if o["kind"] == "chunk":
+            if max_norm is not None and o["kind"] == "chunk":
+                hn.hanayo_chunk_adam_step_clipped(adam, clip, self.desc, o["w"], o["master"], o["g"], o["m"], o["v"], stream)
+            elif max_norm is not None:
+                hn.hanayo_adam_step_clipped(adam, clip, dt, o["w"], o["master"], o["g"], o["m"], o["v"], o["g"].numel(), stream)
+            elif o["kind"] == "chunk":
                 hn.hanayo_chunk_adam_step(adam, self.desc, o["w"], o["master"], o["g"], o["m"], o["v"], stream)
             else:
                 hn.hanayo_adam_step(adam, dt, o["w"], o["master"], o["g"], o["m"], o["v"], o["g"].numel(), stream)

@@ -502,6 +502,52 @@ def test_clipped_chunk_update_decays_matrices_only():
             assert torch.equal(got[o:o + c], want[o:o + c]), name
 
 
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+def test_a_rank_updates_with_clipping(dtype):
+    """GpuRank's flush: all its gradients (chunks, tables, final LayerNorm) under one norm; every parameter moves as the oracle's Adam
+    moves it with the scaled gradient.  A first step moves a parameter by lr g / (|g| + eps'), whose fp32 error is within 16
+    steps of lr, and the parameter is rounded once (its master copy to fp32)."""
+    from paper_2308_15762_amd import synth
+    from paper_2308_15762_amd.runner import GpuRank
+    wl = synth.WORKLOADS["tiny_gpt_fp32"].scaled(dtype=dtype, hidden=64, ffn=128, seq=32)
+    lr, b1, b2, eps, wd = 2.0 ** -8, 0.875, 0.9375, 1e-8, 0.125
+
+    def ready():
+        gpu = GpuRank(wl, 0, ends=True)
+        gpu.zero_grads()
+        gpu.run()
+        gpu.init_optimizer()
+        return gpu
+
+    gpu = ready()
+    grads = [o["g"].double().cpu().numpy().ravel() for o in gpu.opt]
+    before = [(o["w"] if o["master"] is None else o["master"]).double().cpu().numpy().ravel() for o in gpu.opt]
+    norm = OT.grad_norm(grads)
+    limit = float(np.float32(norm / 3))
+    gpu.adam_step(lr, b1, b2, eps, wd, max_norm=limit)
+    assert abs(float(gpu.grad_norm) - norm) <= 1.01 * U * norm
+    k = OT.clip_scale(norm, limit)
+    matrices = np.zeros(grads[0].size, dtype=bool)
+    for blk in range(wl.n_blocks):
+        for i, name in enumerate(hn.PARAM_NAMES):
+            if name in ("wqkv", "wo", "w1", "w2"):
+                off, cnt = hn.hanayo_param_span(gpu.desc, blk, i)
+                matrices[off:off + cnt] = True
+    for o, g, p in zip(gpu.opt, grads, before):
+        decay = matrices if o["kind"] == "chunk" else np.full(g.size, o["kind"] != "lnf")
+        z = np.zeros_like(g)
+        with_wd, plain = (OE.adam_step(p, k * g, z, z, 1, lr, b1, b2, eps, w)[0] for w in (wd, 0.0))
+        want = np.where(decay, with_wd, plain)
+        got = (o["w"] if o["master"] is None else o["master"]).view(-1)
+        near(got, want, 2 * U * np.abs(p) + 16 * U * lr * (1 + wd * np.abs(p)), o["kind"])
+        assert not o["g"].any()
+    # the same limit on the norm of two ranks together: this one's and another that is three times as large
+    two = ready()
+    parts = torch.cat([two.grad_sumsq(), 9 * two.grad_sumsq()])
+    two.adam_step(lr, b1, b2, eps, wd, max_norm=limit, sumsq=parts)
+    assert abs(float(two.grad_norm) - 10 ** 0.5 * norm) <= 4 * U * 10 ** 0.5 * norm
+
+
 # ------------------------------------------------------------------ as they are used together
 
 class Iteration:
