@@ -105,6 +105,32 @@ def test_embedding_backward(dtype, kind, rows, H, vocab):
     assert torch.equal(first, embedding_backward(dtype, tok, dout, 1.5, base, rows, H, vocab, False))     # bit for bit
 
 
+# (rows, columns, vocabulary) on both sides of every choice: one launch up to 1024 rows and 8192 tokens times slabs of 512
+# columns; comparison of all pairs up to 12288 rows; one, two and three digits of the radix sort; pieces of 8 to 64 rows
+BORDERS = [(1024, 512, 8192), (1024, 520, 4097), (1025, 8, 10), (12288, 8, 99), (12289, 8, 99), (12289, 8, 511), (12300, 8, 512),
+           (13000, 8, 262143), (13001, 8, 300000), (40000, 1040, 50), (70000, 2056, 40), (150001, 1024, 600)]
+
+
+@pytest.mark.parametrize("kind", ["half", "zipf"])
+@pytest.mark.parametrize("rows,H,vocab", BORDERS)
+def test_embedding_backward_at_the_borders_of_its_variants(kind, rows, H, vocab):
+    """Also a batch of which half is one token (padding by a token of the vocabulary), and what lies behind the workspace."""
+    rng = np.random.default_rng(rows + vocab)
+    tok = tokens_of("zipf", rng, rows, vocab)
+    if kind == "half":
+        tok[rng.permutation(rows)[:rows // 2]] = vocab // 2
+    dout = torch.randint(-8, 9, (rows, H), device="cuda").to(torch.bfloat16)      # whole numbers: every sum is exact
+    t = torch.from_numpy(tok).cuda()
+    want = torch.zeros((vocab, H), dtype=torch.float64, device="cuda").index_add_(0, t, dout.double())
+    need = hn.hanayo_op_embedding_workspace_bytes(rows, H, vocab)
+    work = room(need + 512)
+    for accumulate in (True, False):
+        d = torch.full((vocab, H), 3.0, device="cuda")
+        hn.hanayo_op_embedding_backward(hn.BF16, t.int(), dout, 0.5, d, rows, H, vocab, accumulate, work)
+        assert torch.equal(d.double(), 0.5 * want + (3.0 if accumulate else 0.0))
+        assert (work[need:] == 0xA5).all()
+
+
 def test_embedding_without_rows():
     e = torch.empty(0, device="cuda")
     t = torch.empty(0, dtype=torch.int32, device="cuda")
@@ -262,7 +288,8 @@ def test_residual_kinds(dtype, post, pre, gate):
 
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
 @pytest.mark.parametrize("rows,H", [(1, 8), (1, 4096), (3, 512), (7, 520), (2, 1016), (130, 1032), (33, 2056), (9, 2560), (11, 3584),
-                                    (517, 4096), (300, 1528), (4500, 64), (2100, 1024), (700, 4088)])
+                                    (517, 4096), (300, 1528), (4500, 64), (2100, 1024), (700, 4088), (1100, 2048), (1030, 2560), (600, 2568),
+                                    (5, 1280), (5, 1288)])
 def test_residual_sizes(dtype, rows, H):
     run_join(Join(dtype, rows, H, "layer", "rms", "channel"))
     run_join(Join(dtype, rows, H, "rms", "layer", "element", seed=1), accumulate=True)
@@ -315,6 +342,40 @@ def test_residual_without_rows():
         x_out, h, st = j.forward()
         got = j.backward(x_out, st, j.dxo, accumulate, 2.0)
         assert all((t == left).all() for t in got[2:])
+
+
+def test_residual_past_32_bit_offsets():
+    """2^31 elements and more: the last rows come out as they do alone."""
+    H, n = 4096, 5
+    rows = (1 << 31) // H + n
+    j = Join("bf16", n, H, "rms", "layer", "element")
+    x_out, h, st = j.forward()
+    alone = j.backward(x_out, st, j.dxo)
+
+    def wide(t):
+        out = torch.zeros((rows, t.shape[1]), dtype=t.dtype, device="cuda")
+        out[-n:] = t
+        return out
+
+    big = Join("bf16", 1, H, "rms", "layer", "element")
+    big.rows, big.desc.rows = rows, rows
+    big.post, big.pre = j.post, j.pre
+    big.x, big.branch, big.gate, big.dh = wide(j.x), wide(j.branch), wide(j.gate), wide(j.dh)
+    bx, bh, bst = big.forward()
+    assert torch.equal(bx[-n:], x_out) and torch.equal(bh[-n:], h) and torch.equal(bst[-n:], st)
+    got = big.backward(bx, bst, wide(j.dxo))
+    assert all(torch.equal(g[-n:], a) for g, a in zip(got[:3], alone[:3]))
+
+
+@pytest.mark.parametrize("rows,H", [(1, 8), (37, 264), (3000, 512), (300, 4096)])
+@pytest.mark.parametrize("pre", ["none", "rms"])
+def test_residual_scratch_is_as_large_as_it_says(rows, H, pre):
+    j = Join("fp32", rows, H, "layer", pre, "channel")
+    x_out, h, st = j.forward()
+    need = hn.hanayo_op_residual_scratch_bytes(j.desc)
+    scratch = room(need + 512)
+    j.backward(x_out, st, j.dxo, scratch=scratch)
+    assert (scratch[need:] == 0xA5).all()
 
 
 def test_residual_repeats_bit_for_bit():
@@ -426,6 +487,27 @@ def test_a_norm_that_is_not_finite_shows_and_changes_nothing(bad):
         n.zero_()
         hn.hanayo_adam_step_clipped(hn.Adam(0.1, 0.9, 0.999, 1e-8, 0.1, 1, zero), hn.make_clip(s, 1, 0.5, n), hn.FP32, p, None, gr, m, v, 16)
         assert (p == 1).all() and (m == 2).all() and (v == 3).all() and (gr == 1 - zero).all() and not np.isfinite(float(n))
+
+
+def test_norm_past_32_bit_offsets():
+    g = torch.zeros((1 << 31) + 77, device="cuda")
+    g[-3:] = torch.tensor([1.0, -2.0, 4.0])
+    g[5] = 8.0
+    lst, s = sumsq_of([g[1:], g[:3]])
+    assert float(s) == 85.0
+    hn.hanayo_op_grad_clip(lst, hn.make_clip(s, 1, float(np.float32(85.0 ** 0.5 / 2))))
+    near(g[-3:], np.array([0.5, -1.0, 2.0]), 4 * U * np.array([1.0, 2.0, 4.0]), "clipped")
+    assert int(torch.count_nonzero(g)) == 4
+
+
+@pytest.mark.parametrize("n", [0, 1, 100, 101, 350])
+def test_norm_workspace_is_as_large_as_it_says(n):
+    grads = [torch.ones(40000 + i, device="cuda") for i in range(n)]
+    need = hn.hanayo_op_grad_workspace_bytes(n)
+    work = room(need + 512)
+    s = torch.zeros(1, dtype=torch.float64, device="cuda")
+    hn.hanayo_op_grad_sumsq(hn.grad_list(grads), s, work)
+    assert float(s) == sum(g.numel() for g in grads) and (work[need:] == 0xA5).all()
 
 
 def test_norm_of_several_ranks():
