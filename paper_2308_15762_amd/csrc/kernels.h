@@ -239,7 +239,7 @@ int embedding_forward(int dtype, const void* table, const int32_t* tokens, float
                       hipStream_t stream);
 // d_table[v][:] (+)= scale * sum of the rows of dout that hold token v
 constexpr int kEmbeddingMaxRows = 1 << 24;
-size_t embedding_workspace_bytes(int rows, int H);
+size_t embedding_workspace_bytes(int rows, int H, int vocab);
 int embedding_backward(int dtype, const int32_t* tokens, const void* dout, float scale, float* d_table, int rows, int H, int vocab,
                        bool accumulate, void* workspace, hipStream_t stream);
 

@@ -43,7 +43,7 @@ typedef __attribute__((ext_vector_type(4), aligned(4))) int i32x4_any;  // four 
 // few rows: every row counts the rows before it (one launch); many rows: radix sort (two launches for every 9 bits of the vocabulary).
 __device__ __forceinline__ int token_key(const int32_t* tokens, int t, int vocab) { return (int)min((unsigned)tokens[t], (unsigned)vocab); }
 
-// The table's gradient is cleared by workgroups of the first launch, beside those that sort.
+// Memory cleared by workgroups of a launch beside those that sort.
 __device__ __forceinline__ void clear_share(f32x4* out, size_t n, int share, int shares, int threads) {
   const size_t step = (size_t)shares * threads;
 #pragma unroll 4
@@ -113,6 +113,7 @@ struct SortArgs {
   const int32_t* tokens;  // the first pass: keys from the tokens, rows in order; later passes: nullptr
   const int32_t *order_in, *sorted_in;
   int32_t *order_out, *sorted_out, *counts;
+  unsigned char* present;  // the last pass: [vocab], 1 for every token that occurs; else nullptr
   int rows, vocab, each, sorters, shift, bits;
 };
 __device__ __forceinline__ int sort_key(const SortArgs& a, int i) { return a.tokens ? token_key(a.tokens, i, a.vocab) : a.sorted_in[i]; }
@@ -134,14 +135,10 @@ __global__ __launch_bounds__(256) void sort_count_kernel(SortArgs a, f32x4* __re
 // Moves a run's keys to their places: behind the keys of smaller digits and those of the same digit in earlier runs and earlier
 // wavefronts (a wavefront owns a sixteenth of the run), in order.  64 keys at a time: a ballot for each bit of the digit finds the
 // lanes with the same one.  The counts of all runs are read by all 1024 threads: two digits each, every fourth run.
-__global__ __launch_bounds__(kSortWaves * 64) void sort_place_kernel(SortArgs a, f32x4* __restrict__ clear, size_t clear_n) {
+__global__ __launch_bounds__(kSortWaves * 64) void sort_place_kernel(SortArgs a) {
   __shared__ int at[kSortWaves][kMaxBins];  // where the wavefront's next key of a digit goes
   __shared__ int2 sums[2][4][kMaxBins / 2];  // of each group of runs: keys of a digit in all runs, in earlier runs
   __shared__ int wave_total[kSortWaves];
-  if ((int)blockIdx.x >= a.sorters) {
-    clear_share(clear, clear_n, blockIdx.x - a.sorters, gridDim.x - a.sorters, kSortWaves * 64);
-    return;
-  }
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, bins = 1 << a.bits;
   const int begin = blockIdx.x * a.each, end = min(begin + a.each, a.rows);
   const int share = a.each / kSortWaves, w0 = min(begin + wave * share, end), w1 = min(w0 + share, end);
@@ -211,6 +208,7 @@ __global__ __launch_bounds__(kSortWaves * 64) void sort_place_kernel(SortArgs a,
       const int to = at[wave][digit] + before;  // read by all lanes before the first of them moves the counter on
       a.order_out[to] = a.tokens ? i : a.order_in[i];
       a.sorted_out[to] = key;
+      if (a.present && key < a.vocab) a.present[key] = 1;
     }
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     __builtin_amdgcn_wave_barrier();
@@ -227,16 +225,29 @@ __global__ __launch_bounds__(kSortWaves * 64) void sort_place_kernel(SortArgs a,
 // parts in order: runs that lie within the workgroup's rows are written, and of those that cross its border it leaves its part in
 // memory, in two slots again, which the kernel below adds up.  A piece's tokens and rows lie in the lanes; eight rows are loaded
 // while the eight before them are added.
-constexpr int kPieces = 8;  // of a workgroup
+// Where the table is written whole (`present`), workgroups behind those clear the rows of the tokens that do not occur, a wavefront
+// sixteen tokens.
+constexpr int kPieces = 8, kClearTokens = 16;  // of a workgroup; of a wavefront
 template <typename T, bool ADD>
 __global__ __launch_bounds__(kPieces * 64) void embedding_sum_kernel(const int32_t* __restrict__ order, const int32_t* __restrict__ sorted,
                                                                      const T* __restrict__ dout, float scale,
                                                                      float* __restrict__ d_table, float* __restrict__ partial, int rows,
-                                                                     int H, int vocab, int R, int slabs) {
+                                                                     int H, int vocab, int R, int slabs, int groups,
+                                                                     const unsigned char* __restrict__ present) {
   __shared__ float parts[kPieces][2][512];
   __shared__ int left[kPieces];  // what a piece left: bit 0 slot 0, bit 1 slot 1, bit 2: the run of slot 0 ends in the piece
   __shared__ int run_of[kPieces];  // the token of the piece's first row, that of slot 0
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  if (!ADD && (int)blockIdx.x >= groups * slabs) {
+    const long v0 = ((long)(blockIdx.x - groups * slabs) * kPieces + wave) * kClearTokens;
+    unsigned long long absent = __ballot(lane < kClearTokens && v0 + lane < vocab && !present[min(v0 + lane, (long)vocab - 1)]);
+    for (; absent; absent &= absent - 1) {
+      f32x4* out = reinterpret_cast<f32x4*>(d_table + (size_t)(v0 + __builtin_ctzll(absent)) * H);
+#pragma unroll 4
+      for (int i = lane; i < H / 4; i += 64) put<true>(out + i, f32x4{0.f, 0.f, 0.f, 0.f});
+    }
+    return;
+  }
   // the slabs of a group of pieces follow each other, so that their rows are read at one time
   const int group = blockIdx.x / slabs, slab = blockIdx.x - group * slabs;
   const int c = (slab * 64 + lane) * 8;
@@ -521,9 +532,9 @@ int piece_rows(int rows, int H) {
 }
 
 struct EmbeddingLayout {
-  size_t order[2], sorted[2], counts, partial, bytes;
+  size_t order[2], sorted[2], counts, present, partial, bytes;
 };
-EmbeddingLayout embedding_layout(int rows, int H) {
+EmbeddingLayout embedding_layout(int rows, int H, int vocab) {
   EmbeddingLayout L{};
   size_t at = 0;
   auto take = [&](size_t bytes) {
@@ -537,6 +548,7 @@ EmbeddingLayout embedding_layout(int rows, int H) {
     L.sorted[i] = take((size_t)rows * 4);
   }
   L.counts = take(radix ? (size_t)kMaxSorters * kMaxBins * 4 : 0);
+  L.present = take(radix ? (size_t)vocab : 0);
   const int each = piece_rows(rows, H) * kPieces;
   L.partial = take(((size_t)rows + each - 1) / each * 2 * H * sizeof(float));
   L.bytes = at;
@@ -545,10 +557,11 @@ EmbeddingLayout embedding_layout(int rows, int H) {
 
 template <typename T, bool ADD>
 int embedding_sums(const int32_t* order, const int32_t* sorted, const void* dout, float scale, float* d_table, float* partial, int rows,
-                   int H, int vocab, hipStream_t stream) {
+                   int H, int vocab, const unsigned char* present, hipStream_t stream) {
   const int r = piece_rows(rows, H), each = r * kPieces, groups = (rows + each - 1) / each, slabs = (H + 511) / 512;
-  launch_kernel((embedding_sum_kernel<T, ADD>), dim3((unsigned)((long)groups * slabs)), dim3(kPieces * 64), 0, stream, order, sorted,
-                (const T*)dout, scale, d_table, partial, rows, H, vocab, r, slabs);
+  const long clearers = present ? ((long)vocab + kPieces * kClearTokens - 1) / (kPieces * kClearTokens) : 0;
+  launch_kernel((embedding_sum_kernel<T, ADD>), dim3((unsigned)((long)groups * slabs + clearers)), dim3(kPieces * 64), 0, stream, order, sorted,
+                (const T*)dout, scale, d_table, partial, rows, H, vocab, r, slabs, groups, present);
   if (const int rc = check_launch("embedding_backward (sums)")) return rc;
   if (groups < 2) return HANAYO_OK;  // no border to cross
   launch_kernel((embedding_join_kernel<ADD>), dim3((groups - 1 + kJoinWaves - 1) / kJoinWaves, slabs), dim3(kJoinWaves * 64), 0, stream,
@@ -569,7 +582,7 @@ int embedding_forward(int dtype, const void* table, const int32_t* tokens, float
   return check_launch("embedding_forward");
 }
 
-size_t embedding_workspace_bytes(int rows, int H) { return embedding_layout(rows, H).bytes + 256; }
+size_t embedding_workspace_bytes(int rows, int H, int vocab) { return embedding_layout(rows, H, vocab).bytes + 256; }
 
 int embedding_backward(int dtype, const int32_t* tokens, const void* dout, float scale, float* d_table, int rows, int H, int vocab,
                        bool accumulate, void* workspace, hipStream_t stream) {
@@ -588,15 +601,19 @@ int embedding_backward(int dtype, const int32_t* tokens, const void* dout, float
     return dtype == HANAYO_BF16 ? embedding_direct<bf16>(tokens, dout, scale, d_table, rows, H, vocab, accumulate, stream)
                                 : embedding_direct<float>(tokens, dout, scale, d_table, rows, H, vocab, accumulate, stream);
   char* ws = static_cast<char*>(workspace);
-  const EmbeddingLayout L = embedding_layout(rows, H);
+  const EmbeddingLayout L = embedding_layout(rows, H, vocab);
   auto ints = [&](size_t at) { return reinterpret_cast<int32_t*>(ws + at); };
   int32_t *order = ints(L.order[0]), *sorted = ints(L.sorted[0]);
+  unsigned char* present = nullptr;
   if (rows <= kRankRows) {
+    // few rows touch little of the table: all of it is cleared beside the sort
     const int sorters = (rows + 15) / 16;
-    launch_kernel(token_rank_kernel, dim3(sorters + clearers(clear_n, 1024)), dim3(1024), (size_t)sorters * 64, stream, tokens, rows, vocab, order, sorted, sorters,
-                  clear, clear_n);
+    launch_kernel(token_rank_kernel, dim3(sorters + clearers(clear_n, 1024)), dim3(1024), (size_t)sorters * 64, stream, tokens, rows,
+                  vocab, order, sorted, sorters, clear, clear_n);
     if (const int rc = check_launch("embedding_backward (sort)")) return rc;
   } else {
+    if (!accumulate) present = reinterpret_cast<unsigned char*>(ws + L.present);
+    const size_t present_n = accumulate ? 0 : ((size_t)vocab + 15) / 16;  // the layout rounds up to 256 bytes
     int bits = 1;
     while (bits < 31 && (vocab >> bits)) ++bits;  // the keys are 0 .. vocab
     const int passes = (bits + 8) / 9;
@@ -604,23 +621,18 @@ int embedding_backward(int dtype, const int32_t* tokens, const void* dout, float
     a.tokens = tokens; a.rows = rows; a.vocab = vocab; a.counts = ints(L.counts);
     const int unit = kSortWaves * 64;  // each wavefront's share is whole rounds of 64
     a.each = ((rows + kMaxSorters - 1) / kMaxSorters + unit - 1) / unit * unit;
-    if (a.each < 1024) a.each = 1024;
     a.sorters = (rows + a.each - 1) / a.each;
-    size_t cleared = 0;  // every launch of the sort, which keeps few CUs busy, clears its share of the table
     for (int pass = 0; pass < passes; ++pass) {
       a.shift = pass * bits / passes;
       a.bits = (pass + 1) * bits / passes - a.shift;
       const int to = pass & 1;
       a.order_out = ints(L.order[to]); a.sorted_out = ints(L.sorted[to]);
-      for (int step = 0; step < 2; ++step) {
-        const size_t upto = clear_n * (2 * pass + step + 1) / (2 * passes), n = upto - cleared;
-        if (step == 0)
-          launch_kernel(sort_count_kernel, dim3(a.sorters + clearers(n, 256)), dim3(256), 0, stream, a, clear + cleared, n);
-        else
-          launch_kernel(sort_place_kernel, dim3(a.sorters + clearers(n, kSortWaves * 64)), dim3(kSortWaves * 64), 0, stream, a, clear + cleared, n);
-        if (const int rc = check_launch("embedding_backward (sort)")) return rc;
-        cleared = upto;
-      }
+      a.present = pass == passes - 1 ? present : nullptr;
+      const size_t n = pass == 0 ? present_n : 0;
+      launch_kernel(sort_count_kernel, dim3(a.sorters + clearers(n, 256)), dim3(256), 0, stream, a, reinterpret_cast<f32x4*>(present), n);
+      if (const int rc = check_launch("embedding_backward (sort, count)")) return rc;
+      launch_kernel(sort_place_kernel, dim3(a.sorters), dim3(kSortWaves * 64), 0, stream, a);
+      if (const int rc = check_launch("embedding_backward (sort, place)")) return rc;
       a.tokens = nullptr;
       a.order_in = a.order_out; a.sorted_in = a.sorted_out;
     }
@@ -629,10 +641,10 @@ int embedding_backward(int dtype, const int32_t* tokens, const void* dout, float
   }
   float* partial = reinterpret_cast<float*>(ws + L.partial);
   if (dtype == HANAYO_BF16)
-    return accumulate ? embedding_sums<bf16, true>(order, sorted, dout, scale, d_table, partial, rows, H, vocab, stream)
-                      : embedding_sums<bf16, false>(order, sorted, dout, scale, d_table, partial, rows, H, vocab, stream);
-  return accumulate ? embedding_sums<float, true>(order, sorted, dout, scale, d_table, partial, rows, H, vocab, stream)
-                    : embedding_sums<float, false>(order, sorted, dout, scale, d_table, partial, rows, H, vocab, stream);
+    return accumulate ? embedding_sums<bf16, true>(order, sorted, dout, scale, d_table, partial, rows, H, vocab, nullptr, stream)
+                      : embedding_sums<bf16, false>(order, sorted, dout, scale, d_table, partial, rows, H, vocab, present, stream);
+  return accumulate ? embedding_sums<float, true>(order, sorted, dout, scale, d_table, partial, rows, H, vocab, nullptr, stream)
+                    : embedding_sums<float, false>(order, sorted, dout, scale, d_table, partial, rows, H, vocab, present, stream);
 }
 
 }  // namespace k

@@ -107,7 +107,7 @@ int hanayo_op_embedding_forward(int dtype, const void* table, const int32_t* tok
 
 size_t hanayo_op_embedding_workspace_bytes(int rows, int hidden, int vocab) {
   if (check_embedding("op_embedding_workspace_bytes", HANAYO_FP32, 1.f, rows, hidden, vocab)) return 0;
-  return k::embedding_workspace_bytes(rows, hidden);
+  return k::embedding_workspace_bytes(rows, hidden, vocab);
 }
 
 int hanayo_op_embedding_backward(int dtype, const int32_t* tokens, const void* dout, float scale, float* d_table, int rows,
