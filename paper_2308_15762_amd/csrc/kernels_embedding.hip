@@ -522,8 +522,8 @@ int embedding_direct(const int32_t* tokens, const void* dout, float scale, float
 // 15.5 us against 25.5 with the radix sort, 8192 rows 22.6 against 30.8, 12288 rows 30.0 against 32.1).
 constexpr int kRankRows = 12288;
 
-// Rows of a piece: enough pieces for four wavefronts on every SIMD where the rows allow it (65521 rows of 1024, first of their
-// iteration: 16 rows 79 us, 32 rows 87, 8 rows 82; 4096 rows: 8 rows 17, 16 rows 20, 32 rows 27).
+// Rows of a piece: enough pieces for four wavefronts on every SIMD where the rows allow it (whole call, 65521 rows of 1024,
+// table written: 16 rows 76.8 us, 8 rows 77.9, 32 rows 85, 64 rows 98; 4096 rows, added: 8 rows 17.5, 16 rows 20.2, 32 rows 27.8).
 int piece_rows(int rows, int H) {
   const long slabs = (H + 511) / 512;
   for (int r = 64; r > 8; r /= 2)

@@ -59,12 +59,16 @@ struct TensorFinder {
   }
 };
 
-__device__ __forceinline__ double sum_256(double v, double* red) {  // red: [4]; the same sum in every thread
+template <int WAVES>
+__device__ __forceinline__ double workgroup_sum(double v, double* red) {  // red: [WAVES]; the same sum in every thread
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, kWave);
   if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
   __syncthreads();
-  return red[0] + red[1] + red[2] + red[3];
+  v = red[0];
+#pragma unroll
+  for (int w = 1; w < WAVES; ++w) v += red[w];
+  return v;
 }
 
 // Elements of a tile before its first 16-byte boundary, and whole vectors behind that; a thread takes vector `thread + 256 u`.
@@ -127,16 +131,16 @@ __global__ __launch_bounds__(256) void grad_sumsq_kernel(GradTable t, double* __
     if (tile < t.keep) acc += e.bf16 ? tile_sumsq<bf16, true>(e, tile) : tile_sumsq<float, true>(e, tile);
     else acc += e.bf16 ? tile_sumsq<bf16, false>(e, tile) : tile_sumsq<float, false>(e, tile);
   }
-  acc = sum_256(acc, red);
+  acc = workgroup_sum<4>(acc, red);
   if (threadIdx.x == 0) partial[blockIdx.x] = acc;
 }
 
-__global__ __launch_bounds__(256) void grad_finish_kernel(const double* __restrict__ partial, size_t n, double* __restrict__ sumsq) {
-  __shared__ double red[4];
+__global__ __launch_bounds__(1024) void grad_finish_kernel(const double* __restrict__ partial, size_t n, double* __restrict__ sumsq) {
+  __shared__ double red[16];
   double acc = 0.0;
-#pragma unroll 8
-  for (size_t i = threadIdx.x; i < n; i += 256) acc += partial[i];
-  acc = sum_256(acc, red);
+#pragma unroll 2
+  for (size_t i = threadIdx.x; i < n; i += 1024) acc += partial[i];  // a launch leaves at most 2048
+  acc = workgroup_sum<16>(acc, red);
   if (threadIdx.x == 0) sumsq[0] = acc;
 }
 
@@ -215,7 +219,7 @@ int grad_sumsq(const hanayo_grad* grads, size_t n, double* sumsq, double* worksp
     if (const int rc = check_launch("grad_sumsq")) return rc;
     partials += blocks;
   }
-  launch_kernel(grad_finish_kernel, dim3(1), dim3(256), 0, stream, workspace, partials, sumsq);
+  launch_kernel(grad_finish_kernel, dim3(1), dim3(1024), 0, stream, workspace, partials, sumsq);
   return check_launch("grad_sumsq (finish)");
 }
 
