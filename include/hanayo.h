@@ -681,7 +681,7 @@ int hanayo_op_colsum_add(int dtype, const void* in, int rows, int n, float* out,
  *   tokens   device int32 [rows]; a token outside [0, vocab) gives a row of zeros, and its row of dout is not read
  *   table    device [vocab][hidden] storage type;  d_table fp32, added to or (accumulate = 0) written whole: what
  *            the first micro-batch of an iteration uses, in place of clearing the table
- *   rows     0 .. 2^24;  hidden a multiple of 8, at most 65536;  row tensors and workspace on 16-byte boundaries
+ *   rows     0 .. 2^24;  hidden a multiple of 8, at most 65536;  vocab at most 2^28;  row tensors and workspace on 16-byte boundaries
  *   workspace  device, hanayo_op_embedding_workspace_bytes(); calls that may overlap need one each; nothing to clear
  */
 int hanayo_op_embedding_forward(int dtype, const void* table, const int32_t* tokens, float scale, void* out, int rows,
@@ -700,7 +700,7 @@ int hanayo_op_embedding_backward(int dtype, const int32_t* tokens, const void* d
 enum { HANAYO_NORM_NONE = 0, HANAYO_NORM_LAYER = 1, HANAYO_NORM_RMS = 2 };
 enum { HANAYO_GATE_NONE = 0, HANAYO_GATE_CHANNEL = 1, HANAYO_GATE_ELEMENT = 2 };
 typedef struct hanayo_residual_desc {
-  int rows;      /* >= 0 */
+  int rows;      /* 0 .. 2^30 */
   int hidden;    /* H; multiple of 8, at most 4096 */
   int dtype;     /* of all row tensors, parameters and the gate */
   int post_norm; /* HANAYO_NORM_* behind the sub-layer */

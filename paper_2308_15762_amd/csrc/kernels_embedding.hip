@@ -4,7 +4,9 @@
 //
 // Both are bound by HBM where they are large and by their launches where they are small.  The gradient first sorts the rows by
 // token (ties in row order), so that the rows of a token follow each other and are added in a fixed order without
-// atomics, whatever the distribution of the tokens.
+// atomics, whatever the distribution of the tokens.  MI355X, bf16: lookup of 4096 rows of 1024 4.0 us; gradient of 65521 such rows, a
+// quarter of them padding, 30592 tokens, written whole: sort 24 us in four launches, sums and clearing 47.7 us (226 MB, 4.7 TB/s; rows in
+// random order alone cost 13 % of a copy's rate), borders 6.9 us.
 #include "device_util.h"
 #include "kernels.h"
 
@@ -39,15 +41,15 @@ typedef __attribute__((ext_vector_type(4))) int i32x4;
 typedef __attribute__((ext_vector_type(4), aligned(4))) int i32x4_any;  // four tokens, on any token's boundary
 
 // ------------------------------------------------------------------ rows sorted by token
-// Keys are tokens; one outside [0, vocab) counts as `vocab` and goes to the end.  Two ways to the same order:
-// few rows: every row counts the rows before it (one launch); many rows: radix sort (two launches for every 9 bits of the vocabulary).
+// Keys are tokens; one outside [0, vocab) counts as `vocab` and goes to the end.  Two ways to the same order: every row counts the
+// rows before it (few rows, one launch), or a radix sort (many rows, two launches for every 9 bits of the vocabulary).
 __device__ __forceinline__ int token_key(const int32_t* tokens, int t, int vocab) { return (int)min((unsigned)tokens[t], (unsigned)vocab); }
 
 // Memory cleared by workgroups of a launch beside those that sort.
 __device__ __forceinline__ void clear_share(f32x4* out, size_t n, int share, int shares, int threads) {
   const size_t step = (size_t)shares * threads;
 #pragma unroll 4
-  for (size_t i = (size_t)share * threads + threadIdx.x; i < n; i += step) 
+  for (size_t i = (size_t)share * threads + threadIdx.x; i < n; i += step)
     put<true>(out + i, f32x4{0.f, 0.f, 0.f, 0.f});
 }
 
@@ -107,7 +109,8 @@ __global__ __launch_bounds__(1024) void token_rank_kernel(const int32_t* __restr
   }
 }
 
-// Radix sort by one digit: workgroup b owns the b-th run of `each` keys.  `counts` [workgroups][bins]: how often each digit occurs in each run.
+// Radix sort by one digit: workgroup b owns the b-th run of `each` keys.  `counts` [workgroups][bins]: how often each digit occurs in
+// each run.
 constexpr int kMaxBins = 512, kMaxSorters = 256, kSortWaves = 16;
 struct SortArgs {
   const int32_t* tokens;  // the first pass: keys from the tokens, rows in order; later passes: nullptr
@@ -264,7 +267,7 @@ __global__ __launch_bounds__(kPieces * 64) void embedding_sum_kernel(const int32
     const unsigned long long ends = __ballot(lane < n && (lane == n - 1 || tok != next));  // the last rows of runs
     unsigned long long whole = ends;                                                       // of runs that lie in the piece
     bool head = before == first;                                                           // the first run comes from before
-    const bool tail = after == __builtin_amdgcn_readlane(tok, n - 1);                      // the last one goes on
+    const bool tail = live == n && after == __builtin_amdgcn_readlane(tok, n - 1);         // the last one goes on
     if (lane == 0) {
       const bool one = (ends & (ends - 1)) == 0;  // a single run
       left[wave] = (head ? 1 | (one && tail ? 0 : 4) : 0) | (tail && !(one && head) ? 2 : 0);
@@ -345,9 +348,9 @@ __global__ __launch_bounds__(kPieces * 64) void embedding_sum_kernel(const int32
   if (open) mine[ours ? H : 0] = run;
 }
 
-// The runs that cross a border between workgroups of the kernel above (`R` rows each here), each by the wavefront of the piece that it starts in: that piece's slot
-// 1 and slot 0 of the pieces behind it.  Runs over many pieces are listed and then added by all wavefronts of the workgroup, every eighth partial sum
-// each, whose sums are added in order.
+// The runs that cross a border between workgroups of the kernel above, whose rows are a piece here (R of them), each by the
+// wavefront of the piece that it starts in: that piece's slot 1 and slot 0 of the pieces behind it.  Runs over many pieces are listed
+// and then added by all wavefronts of the workgroup, every eighth partial sum each, whose sums are added in order.
 constexpr int kJoinWaves = 8, kJoinAlone = 16;
 struct JoinArgs {
   const int32_t* sorted;
@@ -518,6 +521,7 @@ int embedding_direct(const int32_t* tokens, const void* dout, float scale, float
     launch_kernel((embedding_direct_kernel<T, false>), grid, dim3(256), 0, stream, tokens, (const T*)dout, scale, d_table, rows, H);
   return check_launch("embedding_backward (direct)");
 }
+
 // Up to so many rows the comparison of all pairs is the faster sort, and its keys fit the LDS (512 columns, whole call: 4096 rows
 // 15.5 us against 25.5 with the radix sort, 8192 rows 22.6 against 30.8, 12288 rows 30.0 against 32.1).
 constexpr int kRankRows = 12288;

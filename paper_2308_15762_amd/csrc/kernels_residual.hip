@@ -9,7 +9,9 @@
 //   dx = x_scale D,   dbranch = rstd (b - <b> - fhat <b fhat>),  b = q gamma_post
 //   d_pre  = sum over rows of dh xhat, dh;   d_post = of q fhat, q;   dgate = branch_scale D u (per channel: summed over rows)
 //
-// Everything streams its [rows][H] tensors once and is bound by HBM.
+// Everything streams its [rows][H] tensors once and is bound by HBM.  MI355X, bf16: 4096 rows of 1024 forward 8.3 us (34 MB),
+// backward 17.0 us (50 MB; 4 of them the finaliser); 8192 rows of 4096 with a gate per element backward 107 us (537 MB, 5.0 TB/s, what
+// a large copy reaches).
 #include "device_util.h"
 #include "kernels.h"
 
@@ -18,7 +20,7 @@ namespace k {
 
 namespace {
 
-constexpr int kPartialRows = 256;    // workgroups of the backward pass at most = partial rows of column sums
+constexpr int kPartialRows = 256;  // workgroups of the backward pass at most = partial rows of column sums
 
 // Operands that a call does not have (a norm's parameters, a gate) are read all the same, from a tensor that is there, and replaced
 // by 1 or 0 behind the load: a load inside a branch would have to be waited for where the branch ends, and the loads of a row
@@ -367,7 +369,7 @@ int residual_forward_t(const ResidualArgs& a, hipStream_t stream) {
   const int row_bytes = a.H * (int)sizeof(T);
   const bool shared = row_bytes > 5120;
   const int nv = (a.H + (shared ? 2047 : 511)) / (shared ? 2048 : 512), want = shared ? a.rows : (a.rows + 3) / 4;
-  const int most = shared ? 512 : row_bytes >= 4096 ? 256 : want;
+  const int most = shared ? 512 : row_bytes >= 4096 ? 256 : 1 << 20;  // the last: what a grid can hold
   const dim3 grid(want < most ? want : most), block(256);
 #define LAUNCH(NV, W)                                                                                          \
   do {                                                                                                         \

@@ -31,8 +31,8 @@ int check_embedding(const char* what, int dtype, float scale, int rows, int hidd
   TRY(check_dtype(what, dtype));
   if (rows < 0 || hidden < 8 || hidden % 8 || vocab < 1)
     return set_error(HANAYO_EINVAL, "%s: rows %d, hidden %d (a multiple of 8), vocab %d", what, rows, hidden, vocab);
-  if (rows > k::kEmbeddingMaxRows || hidden > 65536)
-    return set_error(HANAYO_EUNSUPPORTED, "%s: more than %d rows or 65536 columns", what, k::kEmbeddingMaxRows);
+  if (rows > k::kEmbeddingMaxRows || hidden > 65536 || vocab > 1 << 28)
+    return set_error(HANAYO_EUNSUPPORTED, "%s: more than %d rows, 65536 columns or 2^28 tokens", what, k::kEmbeddingMaxRows);
   if (!std::isfinite(scale)) return set_error(HANAYO_EINVAL, "%s: scale is not finite", what);
   return HANAYO_OK;
 }
@@ -44,8 +44,8 @@ int check_residual(const hanayo_residual_desc* d) {
   TRY(check_dtype("residual", d->dtype));
   if (d->rows < 0 || d->hidden < 8 || d->hidden % 8)
     return set_error(HANAYO_EINVAL, "residual: rows %d, hidden %d (a multiple of 8)", d->rows, d->hidden);
-  if (d->hidden > k::kResidualMaxHidden)
-    return set_error(HANAYO_EUNSUPPORTED, "residual: hidden %d > %d", d->hidden, k::kResidualMaxHidden);
+  if (d->hidden > k::kResidualMaxHidden || d->rows > 1 << 30)
+    return set_error(HANAYO_EUNSUPPORTED, "residual: hidden %d > %d, or more than 2^30 rows", d->hidden, k::kResidualMaxHidden);
   for (int kind : {d->post_norm, d->pre_norm})
     if (kind != HANAYO_NORM_NONE && kind != HANAYO_NORM_LAYER && kind != HANAYO_NORM_RMS)
       return set_error(HANAYO_EINVAL, "residual: norm %d", kind);

@@ -25,7 +25,7 @@ def test_embedding_forward():
     for at, bad in ((0, 2), (1, None), (2, None), (3, float("nan")), (3, float("inf")), (4, None), (5, -1), (6, 12), (6, 0), (7, 0),
                     (1, A + 8), (2, B_ + 2), (4, C + 8)):
         refuses(hn.EINVAL, f, *(good[:at] + [bad] + good[at + 1:]))
-    for at, bad in ((5, (1 << 24) + 1), (6, 65544)):
+    for at, bad in ((5, (1 << 24) + 1), (6, 65544), (7, (1 << 28) + 1)):
         refuses(hn.EUNSUPPORTED, f, *(good[:at] + [bad] + good[at + 1:]))
 
 
@@ -58,6 +58,7 @@ def test_residual_forward():
     for kw in BAD_DESCS:
         refuses(hn.EINVAL, f, desc(**kw), *good[1:])
     refuses(hn.EUNSUPPORTED, f, desc(hidden=4104), *good[1:])
+    refuses(hn.EUNSUPPORTED, f, desc(rows=(1 << 30) + 1), *good[1:])
     for at in range(1, 8):                       # every operand is needed, on a 16-byte boundary
         refuses(hn.EINVAL, f, *(good[:at] + [None] + good[at + 1:]))
         refuses(hn.EINVAL, f, *(good[:at] + [good[at] + 8] + good[at + 1:]))
