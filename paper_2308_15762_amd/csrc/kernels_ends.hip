@@ -400,11 +400,10 @@ struct AdamDev {
   ClipArgs clip;
 };
 
-// One vector of the four arrays, the gradient scaled by `scale` first where CLIP is set.  With clipping the arrays pass by the
-// caches (nothing here is read again before the next iteration), which leaves the gradients' first part, kept by the pass that
-// formed their norm, where it is.
-template <typename T, bool CLIP>
-__device__ __forceinline__ void adam_vector(const AdamDev& a, size_t i, float scale) {
+template <typename T>
+__global__ __launch_bounds__(256) void adam_kernel(AdamDev a) {
+  const size_t i = ((size_t)blockIdx.x * 256 + threadIdx.x) * 4;
+  if (i >= a.count) return;
   bool decay = true;
   if (a.block_elems) {
     const size_t pos = i % a.block_elems;
@@ -413,16 +412,12 @@ __device__ __forceinline__ void adam_vector(const AdamDev& a, size_t i, float sc
     for (int r = 0; r < 4; ++r) decay = decay || (pos >= a.lo[r] && pos < a.hi[r]);
   }
   const float wd = decay ? a.weight_decay : 0.f;
-  f32x4 g = fetch<CLIP>(reinterpret_cast<const f32x4*>(a.grads + i));
-  if constexpr (CLIP) {
-#pragma unroll
-    for (int e = 0; e < 4; ++e) g[e] *= scale;
-  }
-  f32x4 m = fetch<CLIP>(reinterpret_cast<const f32x4*>(a.m + i));
-  f32x4 v = fetch<CLIP>(reinterpret_cast<const f32x4*>(a.v + i));
+  const f32x4 g = *reinterpret_cast<const f32x4*>(a.grads + i);
+  f32x4 m = *reinterpret_cast<const f32x4*>(a.m + i);
+  f32x4 v = *reinterpret_cast<const f32x4*>(a.v + i);
   f32x4 p;
   if (a.master) {
-    p = fetch<CLIP>(reinterpret_cast<const f32x4*>(a.master + i));
+    p = *reinterpret_cast<const f32x4*>(a.master + i);
   } else {
 #pragma unroll
     for (int e = 0; e < 4; ++e) p[e] = ld(static_cast<const T*>(a.params) + i + e);
@@ -434,27 +429,59 @@ __device__ __forceinline__ void adam_vector(const AdamDev& a, size_t i, float sc
     const float mhat = m[e] * a.corr1, vhat = v[e] * a.corr2;
     p[e] = p[e] - a.lr * (mhat / (sqrtf(vhat) + a.eps) + wd * p[e]);
   }
-  put<CLIP>(reinterpret_cast<f32x4*>(a.m + i), m);
-  put<CLIP>(reinterpret_cast<f32x4*>(a.v + i), v);
-  if (a.master) put<CLIP>(reinterpret_cast<f32x4*>(a.master + i), p);
+  *reinterpret_cast<f32x4*>(a.m + i) = m;
+  *reinterpret_cast<f32x4*>(a.v + i) = v;
+  if (a.master) *reinterpret_cast<f32x4*>(a.master + i) = p;
   if constexpr (sizeof(T) == 2) {
     bf16x4 o;
 #pragma unroll
     for (int e = 0; e < 4; ++e) o[e] = (bf16)p[e];
-    put<CLIP>(reinterpret_cast<bf16x4*>(static_cast<bf16*>(a.params) + i), o);
+    *reinterpret_cast<bf16x4*>(static_cast<bf16*>(a.params) + i) = o;
   } else {
-    put<CLIP>(reinterpret_cast<f32x4*>(static_cast<float*>(a.params) + i), p);
+    *reinterpret_cast<f32x4*>(static_cast<float*>(a.params) + i) = p;
   }
   if (a.zero_grads) *reinterpret_cast<f32x4*>(a.grads + i) = f32x4{0.f, 0.f, 0.f, 0.f};
 }
 
+// With clipping: one vector of the four arrays, the gradient scaled first.  The arrays pass by the caches (nothing here is read again
+// before the next iteration), which leaves the gradients' first part, kept by the pass that formed their norm, where it is.
 template <typename T>
-__global__ __launch_bounds__(256) void adam_kernel(AdamDev a) {
-  const size_t i = ((size_t)blockIdx.x * 256 + threadIdx.x) * 4;
-  if (i < a.count) adam_vector<T, false>(a, i, 1.f);
+__device__ __forceinline__ void adam_clip_vector(const AdamDev& a, size_t i, float scale) {
+  bool decay = true;
+  if (a.block_elems) {
+    const size_t pos = i % a.block_elems;
+    decay = false;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) decay = decay || (pos >= a.lo[r] && pos < a.hi[r]);
+  }
+  const float wd = decay ? a.weight_decay : 0.f;
+  const f32x4 g = fetch<true>(reinterpret_cast<const f32x4*>(a.grads + i));
+  f32x4 m = fetch<true>(reinterpret_cast<const f32x4*>(a.m + i));
+  f32x4 v = fetch<true>(reinterpret_cast<const f32x4*>(a.v + i));
+  f32x4 p = fetch<true>(reinterpret_cast<const f32x4*>((a.master ? a.master : static_cast<const float*>(a.params)) + i));
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const float ge = g[e] * scale;
+    m[e] = a.beta1 * m[e] + (1.f - a.beta1) * ge;
+    v[e] = a.beta2 * v[e] + (1.f - a.beta2) * ge * ge;
+    const float mhat = m[e] * a.corr1, vhat = v[e] * a.corr2;
+    p[e] = p[e] - a.lr * (mhat / (sqrtf(vhat) + a.eps) + wd * p[e]);
+  }
+  put<true>(reinterpret_cast<f32x4*>(a.m + i), m);
+  put<true>(reinterpret_cast<f32x4*>(a.v + i), v);
+  if constexpr (sizeof(T) == 2) {
+    put<true>(reinterpret_cast<f32x4*>(a.master + i), p);
+    bf16x4 o;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) o[e] = (bf16)p[e];
+    put<true>(reinterpret_cast<bf16x4*>(static_cast<bf16*>(a.params) + i), o);
+  } else {
+    put<true>(reinterpret_cast<f32x4*>(static_cast<float*>(a.params) + i), p);
+  }
+  if (a.zero_grads) *reinterpret_cast<f32x4*>(a.grads + i) = f32x4{0.f, 0.f, 0.f, 0.f};
 }
 
-// With clipping a workgroup forms the factor once and walks the arrays with it.  A norm that is not finite leaves parameters
+// A workgroup forms the factor once and walks the arrays with it.  A norm that is not finite leaves parameters
 // and moments as they are (the gradients are still cleared if they are to be).
 template <typename T>
 __global__ __launch_bounds__(256) void adam_clip_kernel(AdamDev a) {
@@ -462,7 +489,7 @@ __global__ __launch_bounds__(256) void adam_clip_kernel(AdamDev a) {
   if (a.clip.norm && blockIdx.x == 0 && threadIdx.x == 0) a.clip.norm[0] = s.norm;
   const size_t stride = (size_t)gridDim.x * 1024;
   for (size_t i = ((size_t)blockIdx.x * 256 + threadIdx.x) * 4; i < a.count; i += stride) {
-    if (s.finite) adam_vector<T, true>(a, i, s.scale);
+    if (s.finite) adam_clip_vector<T>(a, i, s.scale);
     else if (a.zero_grads) *reinterpret_cast<f32x4*>(a.grads + i) = f32x4{0.f, 0.f, 0.f, 0.f};
   }
 }
