@@ -234,14 +234,18 @@ def _room(what, t, count, size):
     that is not on the current device, not contiguous, of another element size or too small is refused."""
     if t is None or type(t) is int:
         return t
+    # one pass over what is asked of a tensor (0.4 us each, of calls of 6 us); what was wrong is found out afterwards
+    try:
+        if 0 <= t.get_device() == _current_device() and t.is_contiguous() and t.element_size() == size and t.numel() >= count:
+            return t.data_ptr()
+    except AttributeError:  # no tensor
+        pass
     if not isinstance(t, torch.Tensor) or not t.is_cuda or not t.is_contiguous():
         raise HanayoError(EINVAL, "%s: a contiguous tensor on the GPU is wanted" % what)
-    if t.element_size() != size or t.numel() < count:
-        raise HanayoError(EINVAL, "%s: %d elements of %d bytes are wanted, not %d of %d"
-                          % (what, count, size, t.numel(), t.element_size()))
     if t.get_device() != _current_device():
         raise HanayoError(EINVAL, "%s: the tensor is not on the current device" % what)
-    return t.data_ptr()
+    raise HanayoError(EINVAL, "%s: %d elements of %d bytes are wanted, not %d of %d"
+                      % (what, count, size, t.numel(), t.element_size()))
 
 
 def make_desc(n_blocks, hidden, heads, ffn, seq, mb, norm, mask, dtype, ln_eps=1e-5):
