@@ -305,7 +305,8 @@ typedef struct hanayo_clip {
   float max_norm;      /* >= 0; infinity never scales */
   float* norm;         /* device float [1], written: the norm before clipping (infinite where fp32 ends); may be NULL */
 } hanayo_clip;
-/* out = grad * scale for every tensor, rounded once to its type.  Where scale is 1, tensors in place are left alone. */
+/* out = grad * scale for every tensor, rounded once to its type.  Where scale is 1, tensors in place are left alone.  No two of the
+   written tensors may overlap (a gradient that two names share is listed once). */
 int hanayo_op_grad_clip(const hanayo_grad* grads, size_t n, const hanayo_clip* clip, void* hip_stream);
 /* hanayo_adam_step and hanayo_chunk_adam_step with grads * scale for grads (the gradients themselves are left as they are,
    or cleared with zero_grads). */
@@ -683,6 +684,7 @@ int hanayo_op_colsum_add(int dtype, const void* in, int rows, int n, float* out,
  *            the first micro-batch of an iteration uses, in place of clearing the table
  *   rows     0 .. 2^24;  hidden a multiple of 8, at most 65536;  vocab at most 2^28;  row tensors and workspace on 16-byte boundaries
  *   workspace  device, hanayo_op_embedding_workspace_bytes(); calls that may overlap need one each; nothing to clear
+ * No two tensors of a call may overlap.
  */
 int hanayo_op_embedding_forward(int dtype, const void* table, const int32_t* tokens, float scale, void* out, int rows,
                                 int hidden, int vocab, void* hip_stream);

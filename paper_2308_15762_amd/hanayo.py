@@ -519,6 +519,10 @@ class GradList:
             self.array[i] = Grad(_room("tensor %d" % i, g, n, e), _room("output %d" % i, out, n, e), n,
                                  BF16 if g.dtype == torch.bfloat16 else FP32)
         self.count = len(grads)
+        # tensors that would be written twice (a gradient listed under two names): their norm can be formed, clipping is refused
+        ends = sorted((t.data_ptr(), t.data_ptr() + t.numel() * t.element_size())
+                      for t in (grads if outs is None else [g if o is None else o for g, o in zip(grads, outs)]) if t.numel())
+        self.overlap = any(a[1] > b[0] for a, b in zip(ends, ends[1:]))
 
 
 def grad_list(grads, outs=None):
@@ -544,6 +548,8 @@ def hanayo_op_grad_sumsq(grads, sumsq, workspace, stream=None):
 
 def hanayo_op_grad_clip(grads, clip, stream=None):
     """grads: a GradList; clip: of make_clip."""
+    if grads.overlap:
+        raise HanayoError(EINVAL, "op_grad_clip: two of the tensors share memory and would be scaled twice")
     _check(_lib.hanayo_op_grad_clip(ctypes.addressof(grads.array), grads.count, ctypes.byref(clip), stream))
 
 

@@ -455,6 +455,25 @@ def test_clipping_leaves_the_neighbours_alone():
     assert float(flat.sum()) == 5000 - sum(v.numel() for v in views)
 
 
+def test_tensors_that_share_memory_are_not_clipped():
+    flat = torch.ones(100, device="cuda")
+    other = torch.zeros(100, device="cuda")
+    for grads, outs, fine in (([flat[:60], flat[59:]], None, False), ([flat, flat], None, False), ([flat[:50], flat[50:]], None, True),
+                              ([flat, flat], [other, other], False), ([flat[:60], flat[40:]], [other[:60], other[60:]], True),
+                              ([flat[:0], flat[:50], flat[10:10]], None, True)):
+        if outs is not None:
+            grads = [g[:o.numel()] for g, o in zip(grads, outs)]
+        lst, s = sumsq_of(grads, outs)
+        assert float(s) == sum(g.numel() for g in grads)          # the norm counts what the list holds
+        if fine:
+            hn.hanayo_op_grad_clip(lst, hn.make_clip(s, 1, 1e9))
+        else:
+            with pytest.raises(hn.HanayoError) as ei:
+                hn.hanayo_op_grad_clip(lst, hn.make_clip(s, 1, 1e9))
+            assert ei.value.code == hn.EINVAL
+    assert (flat == 1).all()
+
+
 @pytest.mark.parametrize("size", [1e30, 3e38, 1e-30, 1e-44])
 def test_norm_of_very_large_and_very_small_gradients(size):
     g = torch.full((3000,), size, device="cuda")
@@ -493,7 +512,7 @@ def test_norm_past_32_bit_offsets():
     g = torch.zeros((1 << 31) + 77, device="cuda")
     g[-3:] = torch.tensor([1.0, -2.0, 4.0])
     g[5] = 8.0
-    lst, s = sumsq_of([g[1:], g[:3]])
+    lst, s = sumsq_of([g[3:], g[:3]])
     assert float(s) == 85.0
     hn.hanayo_op_grad_clip(lst, hn.make_clip(s, 1, float(np.float32(85.0 ** 0.5 / 2))))
     near(g[-3:], np.array([0.5, -1.0, 2.0]), 4 * U * np.array([1.0, 2.0, 4.0]), "clipped")

@@ -96,7 +96,7 @@ def raw_list(*entries):
     arr = (hn.Grad * max(1, len(entries)))(*[hn.Grad(*e) for e in entries])
 
     class L:
-        array, count = arr, len(entries)
+        array, count, overlap = arr, len(entries), False
     return L
 
 
