@@ -78,6 +78,11 @@ int check_grads(const char* what, const hanayo_grad* grads, size_t n, bool outs)
       return set_error(HANAYO_EINVAL, "%s: tensor %zu does not lie on an element's boundary", what, i);
     if (grads[i].count > left) return set_error(HANAYO_EUNSUPPORTED, "%s: more than 2^40 elements", what);
     left -= grads[i].count;
+    if (outs && grads[i].out && grads[i].out != grads[i].grad) {
+      const uintptr_t in = reinterpret_cast<uintptr_t>(grads[i].grad), out = reinterpret_cast<uintptr_t>(grads[i].out);
+      if ((in < out ? out - in : in - out) < grads[i].count * size)
+        return set_error(HANAYO_EINVAL, "%s: tensor %zu overlaps its own output", what, i);
+    }
   }
   return HANAYO_OK;
 }

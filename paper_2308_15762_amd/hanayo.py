@@ -502,6 +502,18 @@ def hanayo_op_residual_backward(desc, x_out, branch, gate, post, pre, stats, dh,
         _room("d_pre", d_pre, n_pre, 4), int(accumulate), _room("scratch", scratch, need, 1), stream))
 
 
+def ranges_conflict(spans):
+    """Whether two of the memory ranges (first address, address behind the last, written) overlap, one of them written."""
+    written = touched = 0  # where the ranges up to here end
+    for first, end, write in sorted(s for s in spans if s[1] > s[0]):
+        if first < (touched if write else written):
+            return True
+        touched = max(touched, end)
+        if write:
+            written = max(written, end)
+    return False
+
+
 class GradList:
     """The tensors of a model's gradients, as hanayo_op_grad_sumsq and hanayo_op_grad_clip take them: marshalled once, kept
     for as long as the tensors stay where they are."""
@@ -519,10 +531,15 @@ class GradList:
             self.array[i] = Grad(_room("tensor %d" % i, g, n, e), _room("output %d" % i, out, n, e), n,
                                  BF16 if g.dtype == torch.bfloat16 else FP32)
         self.count = len(grads)
-        # tensors that would be written twice (a gradient listed under two names): their norm can be formed, clipping is refused
-        ends = sorted((t.data_ptr(), t.data_ptr() + t.numel() * t.element_size())
-                      for t in (grads if outs is None else [g if o is None else o for g, o in zip(grads, outs)]) if t.numel())
-        self.overlap = any(a[1] > b[0] for a, b in zip(ends, ends[1:]))
+        # what clipping would write while other workgroups read or write it: the norm can be formed, clipping is refused
+        spans = []
+        for g, o in zip(grads, grads if outs is None else outs):
+            n, at = g.numel() * g.element_size(), g.data_ptr()
+            to = at if o is None else o.data_ptr()
+            spans.append((to, to + n, True))
+            if to != at:
+                spans.append((at, at + n, False))
+        self.overlap = ranges_conflict(spans)
 
 
 def grad_list(grads, outs=None):
@@ -549,7 +566,7 @@ def hanayo_op_grad_sumsq(grads, sumsq, workspace, stream=None):
 def hanayo_op_grad_clip(grads, clip, stream=None):
     """grads: a GradList; clip: of make_clip."""
     if grads.overlap:
-        raise HanayoError(EINVAL, "op_grad_clip: two of the tensors share memory and would be scaled twice")
+        raise HanayoError(EINVAL, "op_grad_clip: a tensor that is written shares memory with another one of the list")
     _check(_lib.hanayo_op_grad_clip(ctypes.addressof(grads.array), grads.count, ctypes.byref(clip), stream))
 
 

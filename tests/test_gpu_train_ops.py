@@ -772,3 +772,21 @@ def test_strided_operands_are_refused():
         with pytest.raises(hn.HanayoError) as ei:
             hn.hanayo_op_embedding_forward(*args)
         assert ei.value.code == hn.EINVAL
+
+
+def test_tensors_that_others_read_are_not_written():
+    """Outputs that lie on another tensor of the list, or on a part of their own: refused before anything is launched."""
+    flat, other = torch.ones(100, device="cuda"), torch.zeros(100, device="cuda")
+    a, b = flat[:50], flat[50:]
+    for grads, outs, fine in (([a, b], [b, other[:50]], False), ([a, b], [other[:50], a], False), ([a, b], [b, a], False),
+                              ([a, b], [None, a], False), ([flat[:60]], [flat[40:]], False), ([flat[40:]], [flat[:60]], False),
+                              ([a, a], [None, other[:50]], False), ([a, a], [other[:50], other[50:]], True), ([a, b], [a, None], True),
+                              ([a, flat[50:50]], [other[:50], flat[20:20]], True), ([a, b], [other[50:], other[:50]], True)):
+        lst, s = sumsq_of(grads, outs)
+        if fine:
+            hn.hanayo_op_grad_clip(lst, hn.make_clip(s, 1, 1e9))
+        else:
+            with pytest.raises(hn.HanayoError) as ei:
+                hn.hanayo_op_grad_clip(lst, hn.make_clip(s, 1, 1e9))
+            assert ei.value.code == hn.EINVAL
+    assert (flat == 1).all()

@@ -144,3 +144,26 @@ def test_operands_have_to_be_on_the_gpu():
     refuses(hn.EINVAL, hn.grad_list, [torch.zeros(4, dtype=torch.float64)])
     refuses(hn.EINVAL, hn.grad_list, [host], [])
     refuses(hn.EINVAL, hn.make_clip, torch.zeros(1, dtype=torch.float64), 1, 1.0)
+
+
+def test_clipping_past_the_tensor_itself():
+    """An output that begins inside its own tensor, or in front of it: other workgroups would read what one has written."""
+    c = hn.hanayo_op_grad_clip
+    for first, to, count, dtype in ((A, A + 4, 2, hn.FP32), (A + 4, A, 2, hn.FP32), (A, A + 1998, 1000, hn.BF16), (A, A + 4, 1 << 39, hn.FP32)):
+        assert "overlaps" in refuses(hn.EINVAL, c, raw_list((B_, None, 3, hn.FP32), (first, to, count, dtype)), hn.make_clip(B_, 1, 1.0))
+
+
+def test_ranges_that_conflict():
+    """Against every pair of ranges looked at by itself."""
+    assert not hn.ranges_conflict([])
+    rng = np.random.default_rng(0)
+    seen = [0, 0]
+    for _ in range(4000):
+        spans = []
+        for _ in range(int(rng.integers(1, 6))):
+            first = int(rng.integers(0, 40))
+            spans.append((first, first + int(rng.integers(0, 12)), bool(rng.integers(0, 2))))
+        want = any(max(a[0], b[0]) < min(a[1], b[1]) and (a[2] or b[2]) for i, a in enumerate(spans) for b in spans[:i])
+        assert hn.ranges_conflict(spans) == want, spans
+        seen[want] += 1
+    assert min(seen) > 500
