@@ -305,9 +305,10 @@ typedef struct hanayo_clip {
   float max_norm;      /* >= 0; infinity never scales */
   float* norm;         /* device float [1], written: the norm before clipping (infinite where fp32 ends); may be NULL */
 } hanayo_clip;
-/* out = grad * scale for every tensor, rounded once to its type.  Where scale is 1, tensors in place are left alone.  A tensor that is
-   written overlaps no other tensor of the call, neither one that is written (a gradient that two names share is listed once) nor
-   one that is read (another's grad); its own grad it may only be, whole. */
+/* out = grad * scale for every tensor: a product in 32 bits (of a factor rounded to 24 bits, whatever its exponent), rounded to the
+   tensor's type.  Where scale is 1, tensors in place are left alone.  A tensor that is written overlaps no other tensor of the
+   call, neither one that is written (a gradient that two names share is listed once) nor one that is read (another's grad); its
+   own grad it may only be, whole. */
 int hanayo_op_grad_clip(const hanayo_grad* grads, size_t n, const hanayo_clip* clip, void* hip_stream);
 /* hanayo_adam_step and hanayo_chunk_adam_step with grads * scale for grads (the gradients themselves are left as they are,
    or cleared with zero_grads). */

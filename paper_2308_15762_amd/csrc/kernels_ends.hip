@@ -446,7 +446,7 @@ __global__ __launch_bounds__(256) void adam_kernel(AdamDev a) {
 // With clipping: one vector of the four arrays, the gradient scaled first.  The arrays pass by the caches (nothing here is read again
 // before the next iteration), which leaves the gradients' first part, kept by the pass that formed their norm, where it is.
 template <typename T>
-__device__ __forceinline__ void adam_clip_vector(const AdamDev& a, size_t i, float scale) {
+__device__ __forceinline__ void adam_clip_vector(const AdamDev& a, size_t i, const ClipScale& k) {
   bool decay = true;
   if (a.block_elems) {
     const size_t pos = i % a.block_elems;
@@ -461,7 +461,7 @@ __device__ __forceinline__ void adam_clip_vector(const AdamDev& a, size_t i, flo
   f32x4 p = fetch<true>(reinterpret_cast<const f32x4*>((a.master ? a.master : static_cast<const float*>(a.params)) + i));
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
-    const float ge = g[e] * scale;
+    const float ge = k(g[e]);
     m[e] = a.beta1 * m[e] + (1.f - a.beta1) * ge;
     v[e] = a.beta2 * v[e] + (1.f - a.beta2) * ge * ge;
     const float mhat = m[e] * a.corr1, vhat = v[e] * a.corr2;
@@ -489,7 +489,7 @@ __global__ __launch_bounds__(256) void adam_clip_kernel(AdamDev a) {
   if (a.clip.norm && blockIdx.x == 0 && threadIdx.x == 0) a.clip.norm[0] = s.norm;
   const size_t stride = (size_t)gridDim.x * 1024;
   for (size_t i = ((size_t)blockIdx.x * 256 + threadIdx.x) * 4; i < a.count; i += stride) {
-    if (s.finite) adam_clip_vector<T>(a, i, s.scale);
+    if (s.finite) adam_clip_vector<T>(a, i, s);
     else if (a.zero_grads) *reinterpret_cast<f32x4*>(a.grads + i) = f32x4{0.f, 0.f, 0.f, 0.f};
   }
 }

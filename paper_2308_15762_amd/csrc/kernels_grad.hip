@@ -149,13 +149,13 @@ __global__ __launch_bounds__(1024) void grad_finish_kernel(const double* __restr
 }
 
 template <typename T>
-__device__ __forceinline__ void tile_scale(const GradEntry& e, unsigned tile, float scale) {
+__device__ __forceinline__ void tile_scale(const GradEntry& e, unsigned tile, const ClipScale& k) {
   using Vec = typename std::conditional<sizeof(T) == 2, bf16x8, f32x4>::type;
   const TileSplit<T> s(e, tile);
   const T* in = static_cast<const T*>(e.in) + s.begin;
   T* out = static_cast<T*>(e.out) + s.begin;
   if ((reinterpret_cast<uintptr_t>(e.in) ^ reinterpret_cast<uintptr_t>(e.out)) & 15u) {  // no boundary in common
-    for (unsigned i = threadIdx.x; i < s.n; i += 256) st(out + i, ld(in + i) * scale);
+    for (unsigned i = threadIdx.x; i < s.n; i += 256) st(out + i, k(ld(in + i)));
     return;
   }
   Vec v[kLoads];
@@ -170,11 +170,11 @@ __device__ __forceinline__ void tile_scale(const GradEntry& e, unsigned tile, fl
     if (at >= s.vecs) break;
     Vec o;
 #pragma unroll
-    for (unsigned j = 0; j < s.kVec; ++j) o[j] = (T)((float)v[u][j] * scale);
+    for (unsigned j = 0; j < s.kVec; ++j) o[j] = (T)k((float)v[u][j]);
     put<true>(reinterpret_cast<Vec*>(out + s.head + at * s.kVec), o);
   }
   const unsigned i = s.loose(threadIdx.x);
-  if (i < s.n) st(out + i, ld(in + i) * scale);
+  if (i < s.n) st(out + i, k(ld(in + i)));
 }
 
 __global__ __launch_bounds__(256) void grad_clip_kernel(GradTable t, ClipArgs c) {
@@ -183,9 +183,9 @@ __global__ __launch_bounds__(256) void grad_clip_kernel(GradTable t, ClipArgs c)
   if (c.norm && blockIdx.x == 0 && threadIdx.x == 0) c.norm[0] = s.norm;
   for (unsigned tile = blockIdx.x; tile < t.tiles; tile += gridDim.x) {
     const GradEntry& e = t.e[find(tile)];
-    if (s.scale == 1.f && e.in == e.out) continue;
-    if (e.bf16) tile_scale<bf16>(e, tile, s.scale);
-    else tile_scale<float>(e, tile, s.scale);
+    if (s.one() && e.in == e.out) continue;
+    if (e.bf16) tile_scale<bf16>(e, tile, s);
+    else tile_scale<float>(e, tile, s);
   }
 }
 

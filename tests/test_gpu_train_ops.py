@@ -790,3 +790,33 @@ def test_tensors_that_others_read_are_not_written():
                 hn.hanayo_op_grad_clip(lst, hn.make_clip(s, 1, 1e9))
             assert ei.value.code == hn.EINVAL
     assert (flat == 1).all()
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("limit", [100.0, 1.0, 1e-20, 1e-38])
+def test_factors_below_the_range_of_fp32(dtype, limit):
+    """The largest gradients under ordinary and small limits: max_norm / norm has few bits in fp32 or none, the product is what it
+    is for any other norm (and a gradient whose product is no fp32 number vanishes)."""
+    limit = float(np.float32(limit))
+    g = torch.full((3000,), 3e38, dtype=TD[dtype], device="cuda")
+    g[1::7], g[2::7] = -2.5e37, 1e-3
+    w = g.double().cpu().numpy()
+    norm = OT.grad_norm([w])
+    k = OT.clip_scale(norm, limit)
+    assert k < 2.0 ** -126
+    out = torch.empty_like(g)
+    lst, s = sumsq_of([g], [out])
+    hn.hanayo_op_grad_clip(lst, hn.make_clip(s, 1, limit))
+    # two roundings of fp32 (the factor, the product) and one to the type, or half a step of its smallest numbers
+    least = 2.0 ** -149 if dtype == "fp32" else 2.0 ** -133
+    near(out, k * w, np.abs(k * w) * (HALF[dtype] + 3 * U) + least, "clipped")
+    hn.hanayo_op_grad_clip(hn.grad_list([g]), hn.make_clip(s, 1, limit))
+    assert torch.equal(g, out)                                         # in place
+    if dtype == "fp32":
+        g = torch.from_numpy(w.astype(np.float32)).cuda()
+        p, m, v = (torch.full((3000,), x, device="cuda") for x in (0.5, 0.0, 0.0))
+        hn.hanayo_adam_step_clipped(hn.Adam(2.0 ** -10, 0.875, 0.9375, 1e-8, 0.125, 1, 0), hn.make_clip(s, 1, limit), hn.FP32, p, None, g,
+                                    m, v, 3000)
+        _, wm, wv = OE.adam_step(np.full(3000, 0.5), k * w, np.zeros(3000), np.zeros(3000), 1, 2.0 ** -10, 0.875, 0.9375, 1e-8, 0.125)
+        near(m, wm, 4 * U * np.abs(k * w) + 2 * least, "m")
+        near(v, wv, 8 * U * (k * w) ** 2 + 2 * least, "v")
