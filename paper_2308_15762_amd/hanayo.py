@@ -229,14 +229,15 @@ def _ptr(t):
 _current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 
 
-def _room(what, t, count, size):
-    """Device address of an operand of `count` elements of `size` bytes: an integer address as it is, None as NULL; a tensor
-    that is not on the current device, not contiguous, of another element size or too small is refused."""
+def _room(what, t, count, kind):
+    """Device address of an operand of `count` elements of the type `kind` (None: bytes, a workspace): an integer address as it is,
+    None as NULL; a tensor that is not on the current device, not contiguous, of another type or too small is refused."""
     if t is None or type(t) is int:
         return t
     # one pass over what is asked of a tensor (0.4 us each, of calls of 6 us); what was wrong is found out afterwards
     try:
-        if 0 <= t.get_device() == _current_device() and t.is_contiguous() and t.element_size() == size and t.numel() >= count:
+        if (0 <= t.get_device() == _current_device() and t.is_contiguous()
+                and (t.dtype is kind or kind is None and t.element_size() == 1) and t.numel() >= count):
             return t.data_ptr()
     except AttributeError:  # no tensor
         pass
@@ -244,8 +245,15 @@ def _room(what, t, count, size):
         raise HanayoError(EINVAL, "%s: a contiguous tensor on the GPU is wanted" % what)
     if t.get_device() != _current_device():
         raise HanayoError(EINVAL, "%s: the tensor is not on the current device" % what)
-    raise HanayoError(EINVAL, "%s: %d elements of %d bytes are wanted, not %d of %d"
-                      % (what, count, size, t.numel(), t.element_size()))
+    raise HanayoError(EINVAL, "%s: %d elements of %s are wanted, not %d of %s"
+                      % (what, count, "a byte" if kind is None else kind, t.numel(), t.dtype))
+
+
+_F32, _F64, _I32 = torch.float32, torch.float64, torch.int32
+
+
+def _storage(dtype):
+    return torch.bfloat16 if dtype == BF16 else _F32
 
 
 def make_desc(n_blocks, hidden, heads, ffn, seq, mb, norm, mask, dtype, ln_eps=1e-5):
@@ -448,8 +456,8 @@ def hanayo_chunk_adam_step(adam, desc, weights, master, grads, m, v, stream=None
 
 
 def hanayo_op_embedding_forward(dtype, table, tokens, scale, out, rows, hidden, vocab, stream=None):
-    e = 2 if dtype == BF16 else 4
-    _check(_lib.hanayo_op_embedding_forward(dtype, _room("table", table, vocab * hidden, e), _room("tokens", tokens, rows, 4),
+    e = _storage(dtype)
+    _check(_lib.hanayo_op_embedding_forward(dtype, _room("table", table, vocab * hidden, e), _room("tokens", tokens, rows, _I32),
                                             scale, _room("out", out, rows * hidden, e), rows, hidden, vocab, stream))
 
 
@@ -461,17 +469,17 @@ def hanayo_op_embedding_workspace_bytes(rows, hidden, vocab):
 
 
 def hanayo_op_embedding_backward(dtype, tokens, dout, scale, d_table, rows, hidden, vocab, accumulate, workspace, stream=None):
-    e = 2 if dtype == BF16 else 4
+    e = _storage(dtype)
     need = _lib.hanayo_op_embedding_workspace_bytes(rows, hidden, vocab)
-    _check(_lib.hanayo_op_embedding_backward(dtype, _room("tokens", tokens, rows, 4), _room("dout", dout, rows * hidden, e), scale,
-                                             _room("d_table", d_table, vocab * hidden, 4), rows, hidden, vocab, int(accumulate),
-                                             _room("workspace", workspace, need, 1), stream))
+    _check(_lib.hanayo_op_embedding_backward(dtype, _room("tokens", tokens, rows, _I32), _room("dout", dout, rows * hidden, e), scale,
+                                             _room("d_table", d_table, vocab * hidden, _F32), rows, hidden, vocab, int(accumulate),
+                                             _room("workspace", workspace, need, None), stream))
 
 
 def _residual_sizes(d):
-    """(element size, elements of a row tensor, of the post-norm's and the pre-norm's parameters, of the gate)."""
+    """(storage type, elements of a row tensor, of the post-norm's and the pre-norm's parameters, of the gate)."""
     n, H = d.rows * d.hidden, d.hidden
-    return (2 if d.dtype == BF16 else 4, n, 2 * H if d.post_norm == NORM_LAYER else H, 2 * H if d.pre_norm == NORM_LAYER else H,
+    return (_storage(d.dtype), n, 2 * H if d.post_norm == NORM_LAYER else H, 2 * H if d.pre_norm == NORM_LAYER else H,
             n if d.gate == GATE_ELEMENT else H)
 
 
@@ -480,7 +488,7 @@ def hanayo_op_residual_forward(desc, x, branch, gate, post, pre, x_out, h, stats
     _check(_lib.hanayo_op_residual_forward(
         ctypes.byref(desc), _room("x", x, n, e), _room("branch", branch, n, e), _room("gate", gate, n_gate, e),
         _room("post", post, n_post, e), _room("pre", pre, n_pre, e), _room("x_out", x_out, n, e), _room("h", h, n, e),
-        _room("stats", stats, 4 * desc.rows, 4), stream))
+        _room("stats", stats, 4 * desc.rows, _F32), stream))
 
 
 def hanayo_op_residual_scratch_bytes(desc):
@@ -496,10 +504,10 @@ def hanayo_op_residual_backward(desc, x_out, branch, gate, post, pre, stats, dh,
     need = _lib.hanayo_op_residual_scratch_bytes(ctypes.byref(desc))
     _check(_lib.hanayo_op_residual_backward(
         ctypes.byref(desc), _room("x_out", x_out, n, e), _room("branch", branch, n, e), _room("gate", gate, n_gate, e),
-        _room("post", post, n_post, e), _room("pre", pre, n_pre, e), _room("stats", stats, 4 * desc.rows, 4), _room("dh", dh, n, e),
+        _room("post", post, n_post, e), _room("pre", pre, n_pre, e), _room("stats", stats, 4 * desc.rows, _F32), _room("dh", dh, n, e),
         _room("dx_out", dx_out, n, e), _room("dx", dx, n, e), _room("dbranch", dbranch, n, e),
-        _room("dgate", dgate, n_gate, e if desc.gate == GATE_ELEMENT else 4), _room("d_post", d_post, n_post, 4),
-        _room("d_pre", d_pre, n_pre, 4), int(accumulate), _room("scratch", scratch, need, 1), stream))
+        _room("dgate", dgate, n_gate, e if desc.gate == GATE_ELEMENT else _F32), _room("d_post", d_post, n_post, _F32),
+        _room("d_pre", d_pre, n_pre, _F32), int(accumulate), _room("scratch", scratch, need, None), stream))
 
 
 def ranges_conflict(spans):
@@ -527,8 +535,8 @@ class GradList:
             out = None if outs is None else outs[i]
             if g.dtype not in (torch.float32, torch.bfloat16) or (out is not None and out.dtype != g.dtype):
                 raise HanayoError(EINVAL, "grad_list: tensor %d: fp32 or bf16, and its output of the same type" % i)
-            n, e = g.numel(), g.element_size()
-            self.array[i] = Grad(_room("tensor %d" % i, g, n, e), _room("output %d" % i, out, n, e), n,
+            n = g.numel()
+            self.array[i] = Grad(_room("tensor %d" % i, g, n, g.dtype), _room("output %d" % i, out, n, g.dtype), n,
                                  BF16 if g.dtype == torch.bfloat16 else FP32)
         self.count = len(grads)
         # what clipping would write while other workgroups read or write it: the norm can be formed, clipping is refused
@@ -547,7 +555,7 @@ def grad_list(grads, outs=None):
 
 
 def make_clip(sumsq, parts, max_norm, norm=None):
-    c = Clip(_room("sumsq", sumsq, parts, 8), parts, max_norm, _room("norm", norm, 1, 4))
+    c = Clip(_room("sumsq", sumsq, parts, _F64), parts, max_norm, _room("norm", norm, 1, _F32))
     c._keep = (sumsq, norm)
     return c
 
@@ -559,8 +567,8 @@ def hanayo_op_grad_workspace_bytes(n):
 def hanayo_op_grad_sumsq(grads, sumsq, workspace, stream=None):
     """grads: a GradList."""
     need = _lib.hanayo_op_grad_workspace_bytes(grads.count)
-    _check(_lib.hanayo_op_grad_sumsq(ctypes.addressof(grads.array), grads.count, _room("sumsq", sumsq, 1, 8),
-                                     _room("workspace", workspace, need, 1), stream))
+    _check(_lib.hanayo_op_grad_sumsq(ctypes.addressof(grads.array), grads.count, _room("sumsq", sumsq, 1, _F64),
+                                     _room("workspace", workspace, need, None), stream))
 
 
 def hanayo_op_grad_clip(grads, clip, stream=None):
@@ -571,17 +579,18 @@ def hanayo_op_grad_clip(grads, clip, stream=None):
 
 
 def hanayo_adam_step_clipped(adam, clip, dtype, params, master, grads, m, v, count, stream=None):
-    e = 2 if dtype == BF16 else 4
+    e = _storage(dtype)
     _check(_lib.hanayo_adam_step_clipped(ctypes.byref(adam), ctypes.byref(clip), dtype, _room("params", params, count, e),
-                                         _room("master", master, count, 4), _room("grads", grads, count, 4),
-                                         _room("m", m, count, 4), _room("v", v, count, 4), count, stream))
+                                         _room("master", master, count, _F32), _room("grads", grads, count, _F32),
+                                         _room("m", m, count, _F32), _room("v", v, count, _F32), count, stream))
 
 
 def hanayo_chunk_adam_step_clipped(adam, clip, desc, weights, master, grads, m, v, stream=None):
-    n, e = _lib.hanayo_grad_bytes(ctypes.byref(desc)) // 4, 2 if desc.dtype == BF16 else 4
+    n, e = _lib.hanayo_grad_bytes(ctypes.byref(desc)) // 4, _storage(desc.dtype)
     _check(_lib.hanayo_chunk_adam_step_clipped(ctypes.byref(adam), ctypes.byref(clip), ctypes.byref(desc),
-                                               _room("weights", weights, n, e), _room("master", master, n, 4),
-                                               _room("grads", grads, n, 4), _room("m", m, n, 4), _room("v", v, n, 4), stream))
+                                               _room("weights", weights, n, e), _room("master", master, n, _F32),
+                                               _room("grads", grads, n, _F32), _room("m", m, n, _F32),
+                                               _room("v", v, n, _F32), stream))
 
 
 def hanayo_op_gemm(dtype, A, B, C, M, N, K, lda, ldb, ldc, a_t, b_t, epilogue, bias=None, aux=None, aux_out=None,

@@ -820,3 +820,40 @@ def test_factors_below_the_range_of_fp32(dtype, limit):
         _, wm, wv = OE.adam_step(np.full(3000, 0.5), k * w, np.zeros(3000), np.zeros(3000), 1, 2.0 ** -10, 0.875, 0.9375, 1e-8, 0.125)
         near(m, wm, 4 * U * np.abs(k * w) + 2 * least, "m")
         near(v, wv, 8 * U * (k * w) ** 2 + 2 * least, "v")
+
+
+def test_operands_of_another_type_are_refused():
+    """Tensors as large as the right ones, of types that other values stand for."""
+    rows, H, V = 8, 16, 8
+    z = lambda dtype, n=256: torch.zeros(n, dtype=dtype, device="cuda")
+    b16, f32, i32, f64 = z(torch.bfloat16), z(torch.float32), z(torch.int32), z(torch.float64)
+    swap = {torch.bfloat16: (z(torch.float16), z(torch.int16)), torch.float32: (i32, z(torch.uint32)), torch.int32: (f32, z(torch.uint32)),
+            torch.float64: (z(torch.int64),)}
+    room_ = z(torch.uint8, 1 << 20)
+    desc = hn.ResidualDesc(rows, H, hn.BF16, hn.NORM_LAYER, hn.NORM_RMS, hn.GATE_CHANNEL, 1.0, 1.0, EPS)
+    r = lambda: z(torch.bfloat16)
+    # every call is right as it stands
+    calls = [(hn.hanayo_op_embedding_forward, [hn.BF16, b16, i32, 1.0, r(), rows, H, V]),
+             (hn.hanayo_op_embedding_forward, [hn.FP32, f32, i32, 1.0, z(torch.float32), rows, H, V]),
+             (hn.hanayo_op_embedding_backward, [hn.BF16, i32, b16, 1.0, f32, rows, H, V, False, room_]),
+             (hn.hanayo_op_residual_forward, [desc, b16, r(), r(), r(), r(), r(), r(), f32]),
+             (hn.hanayo_op_residual_backward, [desc, b16, r(), r(), r(), r(), f32, r(), r(), r(), r(), z(torch.float32), z(torch.float32),
+                                               z(torch.float32), False, room_]),
+             (hn.hanayo_op_grad_sumsq, [hn.grad_list([f32]), f64, room_]),
+             (hn.make_clip, [f64, 1, 1.0, f32]),
+             (hn.hanayo_adam_step_clipped, [hn.Adam(0.1, 0.9, 0.999, 1e-8, 0.1, 1, 0), hn.make_clip(f64, 1, 1.0), hn.BF16, b16, f32,
+                                            z(torch.float32), z(torch.float32), z(torch.float32), 256])]
+    for call, args in calls:
+        call(*args)
+        seen = 0
+        for at, arg in enumerate(args):
+            if isinstance(arg, torch.Tensor) and arg is not room_:
+                for other in swap[arg.dtype]:
+                    with pytest.raises(hn.HanayoError) as ei:
+                        call(*(args[:at] + [other] + args[at + 1:]))
+                    assert ei.value.code == hn.EINVAL
+                    seen += 1
+        assert seen
+    for bad in (z(torch.float16), i32, f64):
+        with pytest.raises(hn.HanayoError):
+            hn.grad_list([bad])
