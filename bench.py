@@ -212,6 +212,8 @@ def main():
                     help="instead of the benchmark: time the plain copy kernel at these sizes (MiB read and as many "
                          "written; default 4 8 16 32 64 256), the yardstick of the memory-bound kernels")
     args = ap.parse_args()
+    if args.max_norm is not None and not args.adam:
+        ap.error("--max-norm clips in the Adam update: it needs --adam")
     if args.gpus != 1:
         sys.exit("bench.py: this build covers one GPU's share of the pipeline (one rank); --gpus must be 1")
 
@@ -243,7 +245,7 @@ def main():
             gpu.zero_grads()
         peak = gpu.run()
         if args.adam:
-            gpu.adam_step(1e-4, weight_decay=0.01, max_norm=args.max_norm)                            # clears the gradients as it goes
+            gpu.adam_step(1e-4, weight_decay=0.01, max_norm=args.max_norm)         # clears the gradients as it goes
         return peak
 
     # one plain copy of known size: the dispatch the HBM traffic counters of a profiler run are scaled by

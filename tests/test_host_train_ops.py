@@ -2,6 +2,9 @@
 every call ends in its argument checks."""
 
 import ctypes
+import os
+import subprocess
+import sys
 
 import numpy as np
 import pytest
@@ -167,3 +170,9 @@ def test_ranges_that_conflict():
         assert hn.ranges_conflict(spans) == want, spans
         seen[want] += 1
     assert min(seen) > 500
+
+
+def test_a_limit_without_an_update_is_refused_by_the_benchmark():
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    r = subprocess.run([sys.executable, os.path.join(root, "bench.py"), "--max-norm", "1.0"], capture_output=True, text=True, timeout=300)
+    assert r.returncode == 2 and "--adam" in r.stderr and not r.stdout
