@@ -285,7 +285,7 @@ int hanayo_chunk_adam_step(const hanayo_adam* o, const hanayo_chunk_desc* d, voi
  *   norm = sqrt(sumsq[0] + .. + sumsq[parts - 1]);  scale = norm > max_norm ? max_norm / norm : 1
  * Squares are formed and added in 64 bits, so no fp32 gradient is too large or too small for them; the order is fixed and
  * results repeat bit for bit.  A norm that is infinite or NaN (a gradient was): hanayo_op_grad_clip takes scale
- * = 1, and the clipped updates leave parameters and moments as they are; either way `norm` shows it.  (A finite
+ * = 1, and the clipped updates leave parameters and moments as they are and count in `skipped`; either way `norm` shows it.  (A finite
  * norm beyond fp32's range, 3.4e38, is infinite in `norm` alone.)
  * ------------------------------------------------------------------------- */
 typedef struct hanayo_grad {
@@ -304,6 +304,10 @@ typedef struct hanayo_clip {
   int parts;           /* 1 where the caller has added them up already */
   float max_norm;      /* >= 0; infinity never scales */
   float* norm;         /* device float [1], written: the norm before clipping (infinite where fp32 ends); may be NULL */
+  int32_t* skipped;    /* the clipped updates only; device int32 [1], 0 before an array's first update: how many of its updates a norm that
+                          is not finite has kept from happening.  Such an update adds one; another one corrects its moments' bias as
+                          update number o->step - skipped, so that o->step may count all of them and the host need not know.  One counter
+                          for each array that is updated by a call of its own; NULL: o->step is the number, whatever happened before. */
 } hanayo_clip;
 /* out = grad * scale for every tensor: a product in 32 bits (of a factor rounded to 24 bits, whatever its exponent), rounded to the
    tensor's type.  Where scale is 1, tensors in place are left alone.  A tensor that is written overlaps no other tensor of the

@@ -199,6 +199,7 @@ struct ClipArgs {
   int parts;
   float max_norm;
   float* norm;  // [1] written: the norm before clipping; may be nullptr
+  int* skipped;  // [1] Adam: updates that did not happen, added to by one that does not; may be nullptr
 };
 struct AdamArgs {
   void* params;   // storage type, updated

@@ -398,6 +398,7 @@ struct AdamDev {
   size_t block_elems;
   size_t lo[4], hi[4];
   ClipArgs clip;
+  int step;  // of the clipped update: t, skipped updates among it
 };
 
 template <typename T>
@@ -446,7 +447,7 @@ __global__ __launch_bounds__(256) void adam_kernel(AdamDev a) {
 // With clipping: one vector of the four arrays, the gradient scaled first.  The arrays pass by the caches (nothing here is read again
 // before the next iteration), which leaves the gradients' first part, kept by the pass that formed their norm, where it is.
 template <typename T>
-__device__ __forceinline__ void adam_clip_vector(const AdamDev& a, size_t i, const ClipScale& k) {
+__device__ __forceinline__ void adam_clip_vector(const AdamDev& a, size_t i, const ClipScale& k, float corr1, float corr2) {
   bool decay = true;
   if (a.block_elems) {
     const size_t pos = i % a.block_elems;
@@ -464,7 +465,7 @@ __device__ __forceinline__ void adam_clip_vector(const AdamDev& a, size_t i, con
     const float ge = k(g[e]);
     m[e] = a.beta1 * m[e] + (1.f - a.beta1) * ge;
     v[e] = a.beta2 * v[e] + (1.f - a.beta2) * ge * ge;
-    const float mhat = m[e] * a.corr1, vhat = v[e] * a.corr2;
+    const float mhat = m[e] * corr1, vhat = v[e] * corr2;
     p[e] = p[e] - a.lr * (mhat / (sqrtf(vhat) + a.eps) + wd * p[e]);
   }
   put<true>(reinterpret_cast<f32x4*>(a.m + i), m);
@@ -481,15 +482,33 @@ __device__ __forceinline__ void adam_clip_vector(const AdamDev& a, size_t i, con
   if (a.zero_grads) *reinterpret_cast<f32x4*>(a.grads + i) = f32x4{0.f, 0.f, 0.f, 0.f};
 }
 
+__device__ float bias_correction(float beta, int t) {  // 1 / (1 - beta^t)
+  double power = 1.0, b = beta;
+  for (; t; t >>= 1, b *= b)
+    if (t & 1) power *= b;
+  return (float)(1.0 / (1.0 - power));
+}
+
 // A workgroup forms the factor once and walks the arrays with it.  A norm that is not finite leaves parameters
-// and moments as they are (the gradients are still cleared if they are to be).
+// and moments as they are (the gradients are still cleared if they are to be) and is counted; a launch either counts, by one thread, or reads
+// the count.
 template <typename T>
 __global__ __launch_bounds__(256) void adam_clip_kernel(AdamDev a) {
   const ClipScale s = clip_scale(a.clip);
   if (a.clip.norm && blockIdx.x == 0 && threadIdx.x == 0) a.clip.norm[0] = s.norm;
+  float corr1 = a.corr1, corr2 = a.corr2;
+  if (a.clip.skipped && !s.finite) {
+    if (blockIdx.x == 0 && threadIdx.x == 0) ++*a.clip.skipped;
+  } else if (a.clip.skipped) {
+    if (const int skipped = __builtin_amdgcn_readfirstlane(*a.clip.skipped)) {
+      const int t = max(a.step - skipped, 1);
+      corr1 = bias_correction(a.beta1, t);
+      corr2 = bias_correction(a.beta2, t);
+    }
+  }
   const size_t stride = (size_t)gridDim.x * 1024;
   for (size_t i = ((size_t)blockIdx.x * 256 + threadIdx.x) * 4; i < a.count; i += stride) {
-    if (s.finite) adam_clip_vector<T>(a, i, s);
+    if (s.finite) adam_clip_vector<T>(a, i, s, corr1, corr2);
     else if (a.zero_grads) *reinterpret_cast<f32x4*>(a.grads + i) = f32x4{0.f, 0.f, 0.f, 0.f};
   }
 }
@@ -603,6 +622,7 @@ int adam(int dtype, const AdamArgs& g, hipStream_t stream) {
   const size_t vec = g.count / 4, blocks = (vec + 255) / 256;
   if (g.clip.sumsq) {
     a.clip = g.clip;
+    a.step = g.step;
     const dim3 grid((unsigned)(blocks < 2048 ? blocks : 2048));  // 8 workgroups on every CU
     if (dtype == HANAYO_BF16) launch_kernel(adam_clip_kernel<bf16>, grid, dim3(256), 0, stream, a);
     else launch_kernel(adam_clip_kernel<float>, grid, dim3(256), 0, stream, a);

@@ -91,8 +91,9 @@ int check_clip(const char* what, const hanayo_clip* c, k::ClipArgs& out) {
   if (!c || !c->sumsq) return set_error(HANAYO_EINVAL, "%s: NULL clip or sumsq", what);
   if (c->parts < 1 || c->parts > 65536) return set_error(HANAYO_EINVAL, "%s: parts %d", what, c->parts);
   if (!(c->max_norm >= 0.f)) return set_error(HANAYO_EINVAL, "%s: max_norm must be >= 0", what);
-  if (off(c->sumsq, 8) || off(c->norm, 4)) return set_error(HANAYO_EINVAL, "%s: misaligned sumsq or norm", what);
-  out = k::ClipArgs{c->sumsq, c->parts, c->max_norm, c->norm};
+  if (off(c->sumsq, 8) || off(c->norm, 4) || off(c->skipped, 4))
+    return set_error(HANAYO_EINVAL, "%s: misaligned sumsq, norm or skipped", what);
+  out = k::ClipArgs{c->sumsq, c->parts, c->max_norm, c->norm, c->skipped};
   return HANAYO_OK;
 }
 

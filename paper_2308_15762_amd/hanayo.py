@@ -107,7 +107,8 @@ class Grad(ctypes.Structure):
 
 
 class Clip(ctypes.Structure):
-    _fields_ = [("sumsq", ctypes.c_void_p), ("parts", ctypes.c_int), ("max_norm", ctypes.c_float), ("norm", ctypes.c_void_p)]
+    _fields_ = [("sumsq", ctypes.c_void_p), ("parts", ctypes.c_int), ("max_norm", ctypes.c_float), ("norm", ctypes.c_void_p),
+                ("skipped", ctypes.c_void_p)]
 
 
 class HanayoError(RuntimeError):
@@ -554,9 +555,9 @@ def grad_list(grads, outs=None):
     return GradList(grads, outs)
 
 
-def make_clip(sumsq, parts, max_norm, norm=None):
-    c = Clip(_room("sumsq", sumsq, parts, _F64), parts, max_norm, _room("norm", norm, 1, _F32))
-    c._keep = (sumsq, norm)
+def make_clip(sumsq, parts, max_norm, norm=None, skipped=None):
+    c = Clip(_room("sumsq", sumsq, parts, _F64), parts, max_norm, _room("norm", norm, 1, _F32), _room("skipped", skipped, 1, _I32))
+    c._keep = (sumsq, norm, skipped)
     return c
 
 

@@ -190,6 +190,9 @@ class GpuRank:
         self.grad_work = dev_bytes(hn.hanayo_op_grad_workspace_bytes(len(self.opt)))
         self.sumsq = torch.zeros(1, dtype=torch.float64, device="cuda")
         self.grad_norm = torch.zeros(1, dtype=torch.float32, device="cuda")
+        # updates that a norm that was not finite kept from happening, counted on the device for every array
+        self.skipped = torch.zeros(len(self.opt), dtype=torch.int32, device="cuda")
+        self.may_have_skipped = False
 
     def grad_sumsq(self, stream=None):
         """The squared norm of all gradients that the rank holds, a float64 tensor on the GPU: what ranks exchange before they clip."""
@@ -202,15 +205,24 @@ class GpuRank:
         Decay goes to the chunks' matrices and the tables, not to biases and LayerNorm parameters.
         max_norm: the gradients are scaled down to this norm on the way; grad_norm then holds the norm before.  sumsq: the
         squared norms of all ranks (float64, on the GPU; default: of this rank alone).  A norm that is not finite leaves parameters
-        and moments as they are."""
-        self.opt_step += 1
+        and moments as they are, and the update does not count in the bias corrections of later ones.  (An update without max_norm takes their
+        number from the host: the first one behind clipped ones waits for the device.)"""
         if max_norm is not None:
             sumsq = self.grad_sumsq(stream) if sumsq is None else sumsq
-            clip = hn.make_clip(sumsq, sumsq.numel(), max_norm, self.grad_norm)
+            clips = [hn.make_clip(sumsq, sumsq.numel(), max_norm, self.grad_norm, self.skipped[i:i + 1]) for i in range(len(self.opt))]
+            self.may_have_skipped = True
+        else:
+            clips = [None] * len(self.opt)
+            if self.may_have_skipped:
+                torch.cuda.synchronize()
+                self.opt_step -= int(self.skipped[0])
+                self.skipped.zero_()
+                torch.cuda.synchronize()
+                self.may_have_skipped = False
         dt = hn.BF16 if self.wl.dtype == "bf16" else hn.FP32
-        for o in self.opt:
+        for o, clip in zip(self.opt, clips):
             wd = 0.0 if o["kind"] == "lnf" else weight_decay
-            adam = hn.Adam(lr, beta1, beta2, eps, wd, self.opt_step, int(zero_grads))
+            adam = hn.Adam(lr, beta1, beta2, eps, wd, self.opt_step + 1, int(zero_grads))
             if max_norm is not None and o["kind"] == "chunk":
                 hn.hanayo_chunk_adam_step_clipped(adam, clip, self.desc, o["w"], o["master"], o["g"], o["m"], o["v"], stream)
             elif max_norm is not None:
@@ -219,6 +231,7 @@ class GpuRank:
                 hn.hanayo_chunk_adam_step(adam, self.desc, o["w"], o["master"], o["g"], o["m"], o["v"], stream)
             else:
                 hn.hanayo_adam_step(adam, dt, o["w"], o["master"], o["g"], o["m"], o["v"], o["g"].numel(), stream)
+        self.opt_step += 1
 
 
 class GpuPipeline:

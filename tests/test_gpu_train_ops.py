@@ -857,3 +857,61 @@ def test_operands_of_another_type_are_refused():
     for bad in (z(torch.float16), i32, f64):
         with pytest.raises(hn.HanayoError):
             hn.grad_list([bad])
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("bad_at", [(0,), (1,), (0, 1, 3)])
+def test_an_update_that_did_not_happen_is_not_counted(dtype, bad_at):
+    """Four updates, some with an infinite gradient among them, against the good ones alone, which count what they are: the same bits."""
+    n, rng = 1028, np.random.default_rng(9)
+    start = [values(rng, n, "fp32", std)[0] for std in (0.02, 0.1, 0.1)]
+    start[2].abs_()
+    grads = [values(rng, n, "fp32", 0.3)[0] for _ in range(4)]
+    s, skipped = torch.zeros(1, dtype=torch.float64, device="cuda"), torch.zeros(2, dtype=torch.int32, device="cuda")
+
+    def run(steps, counter):
+        p, m, v = (t.clone() for t in start)
+        q = p.bfloat16()
+        for step, g in steps:
+            g = g.clone()
+            hn.hanayo_op_grad_sumsq(hn.grad_list([g]), s, room(hn.hanayo_op_grad_workspace_bytes(1)))
+            hn.hanayo_adam_step_clipped(hn.Adam(2.0 ** -8, 0.875, 0.999, 1e-8, 0.125, step, 0), hn.make_clip(s, 1, 1.0, None, counter), DT[dtype],
+                                        q if dtype == "bf16" else p, p if dtype == "bf16" else None, g, m, v, n)
+        return p, q, m, v
+
+    good = [g for i, g in enumerate(grads) if i not in bad_at]
+    for i in bad_at:
+        grads[i] = grads[i].clone()
+        grads[i][77] = float("inf")
+    want = run(list(enumerate(good, 1)), None)
+    got = run(list(enumerate(grads, 1)), skipped[:1])
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    assert skipped.tolist() == [len(bad_at), 0]
+
+
+@pytest.mark.parametrize("mixed", [False, True])
+def test_a_rank_does_not_count_a_flush_that_did_not_happen(mixed):
+    """GpuRank: a flush with an infinite gradient, then a good one (mixed: a clipped and an unclipped one), against the good ones alone."""
+    from paper_2308_15762_amd import synth
+    from paper_2308_15762_amd.runner import GpuRank
+    wl = synth.WORKLOADS["tiny_gpt_fp32"].scaled(hidden=64, ffn=128, seq=32)
+    ends = []
+    for bad in (True, False):
+        gpu = GpuRank(wl, 0, ends=True)
+        gpu.zero_grads()
+        gpu.init_optimizer()
+        if bad:
+            gpu.opt[1]["g"][0] = float("inf")
+            gpu.adam_step(2.0 ** -8, max_norm=0.5)
+            assert not np.isfinite(float(gpu.grad_norm)) and not any(o["m"].any() or o["g"].any() for o in gpu.opt)
+        for limit in (0.5, None) if mixed else (0.5,):
+            gpu.run()
+            gpu.adam_step(2.0 ** -8, max_norm=limit)
+        ends.append(gpu)
+    for a, b in zip(*(g.opt for g in ends)):
+        assert all(torch.equal(a[k], b[k]) for k in ("w", "m", "v"))
+    # a call that is refused counts nothing either
+    before = gpu.opt_step
+    with pytest.raises(hn.HanayoError):
+        gpu.adam_step(2.0 ** -8, max_norm=-1.0)
+    assert gpu.opt_step == before

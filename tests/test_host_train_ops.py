@@ -172,6 +172,13 @@ def test_ranges_that_conflict():
     assert min(seen) > 500
 
 
+def test_the_counter_of_skipped_updates():
+    adam = hn.Adam(1e-3, 0.9, 0.999, 1e-8, 0.0, 1, 0)
+    refuses(hn.EINVAL, hn.hanayo_adam_step_clipped, adam, hn.make_clip(A, 1, 1.0, None, I + 2), hn.BF16, B_, C, D, E, G, 16)
+    refuses(hn.EINVAL, hn.make_clip, A, 1, 1.0, None, torch.zeros(1, dtype=torch.int32))
+    assert hn.Clip(A, 1, 1.0, None).skipped is None
+
+
 def test_a_limit_without_an_update_is_refused_by_the_benchmark():
     root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
     r = subprocess.run([sys.executable, os.path.join(root, "bench.py"), "--max-norm", "1.0"], capture_output=True, text=True, timeout=300)
