@@ -207,6 +207,8 @@ class GpuRank:
         squared norms of all ranks (float64, on the GPU; default: of this rank alone).  A norm that is not finite leaves parameters
         and moments as they are, and the update does not count in the bias corrections of later ones.  (An update without max_norm takes their
         number from the host: the first one behind clipped ones waits for the device.)"""
+        if sumsq is not None and max_norm is None:
+            raise hn.HanayoError(hn.EINVAL, "adam_step: sumsq without max_norm")
         if max_norm is not None:
             sumsq = self.grad_sumsq(stream) if sumsq is None else sumsq
             clips = [hn.make_clip(sumsq, sumsq.numel(), max_norm, self.grad_norm, self.skipped[i:i + 1]) for i in range(len(self.opt))]

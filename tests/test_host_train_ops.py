@@ -179,6 +179,11 @@ def test_the_counter_of_skipped_updates():
     assert hn.Clip(A, 1, 1.0, None).skipped is None
 
 
+def test_norms_without_a_limit_are_refused():
+    from paper_2308_15762_amd.runner import GpuRank
+    refuses(hn.EINVAL, GpuRank.adam_step, None, 1e-3, sumsq=torch.zeros(2, dtype=torch.float64))
+
+
 def test_a_limit_without_an_update_is_refused_by_the_benchmark():
     root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
     r = subprocess.run([sys.executable, os.path.join(root, "bench.py"), "--max-norm", "1.0"], capture_output=True, text=True, timeout=300)
