@@ -181,7 +181,7 @@ def test_the_counter_of_skipped_updates():
 
 def test_norms_without_a_limit_are_refused():
     from paper_2308_15762_amd.runner import GpuRank
-    refuses(hn.EINVAL, GpuRank.adam_step, None, 1e-3, sumsq=torch.zeros(2, dtype=torch.float64))
+    refuses(hn.EINVAL, lambda: GpuRank.adam_step(None, 1e-3, sumsq=torch.zeros(2, dtype=torch.float64)))
 
 
 def test_a_limit_without_an_update_is_refused_by_the_benchmark():
