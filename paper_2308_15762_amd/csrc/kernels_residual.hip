@@ -364,21 +364,29 @@ __global__ __launch_bounds__(1024) void residual_finalize_kernel(ResidualArgs a,
 //   4096 (4096)             36.9 / 39.9 / - (with two 31.5);  37.5 / 28.7 / 29.9
 //   fp32 2048 (8192)        53.5 / 55.8 / -;  63.0 / 51.4 / 62.1
 //   fp32 4096 (4096)        -  ;  55.8 / 52.0 / 61.6
+constexpr int kAloneBytes = 5120;  // of a row that one wavefront takes
 template <typename T>
 int residual_forward_t(const ResidualArgs& a, hipStream_t stream) {
   const int row_bytes = a.H * (int)sizeof(T);
-  const bool shared = row_bytes > 5120;
+  const bool shared = row_bytes > kAloneBytes;
   const int nv = (a.H + (shared ? 2047 : 511)) / (shared ? 2048 : 512), want = shared ? a.rows : (a.rows + 3) / 4;
   const int most = shared ? 512 : row_bytes >= 4096 ? 256 : 1 << 20;  // the last: what a grid can hold
   const dim3 grid(want < most ? want : most), block(256);
-#define LAUNCH(NV, W)                                                                                          \
-  do {                                                                                                         \
-    if (a.H == 512 * NV * W) launch_kernel((residual_fwd_kernel<T, NV, W, true>), grid, block, 0, stream, a);  \
-    else launch_kernel((residual_fwd_kernel<T, NV, W, false>), grid, block, 0, stream, a);                     \
+#define LAUNCH(NV, W)                                                                    \
+  do {                                                                                   \
+    if constexpr (W > 1 || 512 * NV * (int)sizeof(T) <= kAloneBytes) {                   \
+      if (a.H == 512 * NV * W) {                                                         \
+        launch_kernel((residual_fwd_kernel<T, NV, W, true>), grid, block, 0, stream, a); \
+        break;                                                                           \
+      }                                                                                  \
+    }                                                                                    \
+    launch_kernel((residual_fwd_kernel<T, NV, W, false>), grid, block, 0, stream, a);    \
   } while (0)
   if (shared) {
-    if (nv == 1) LAUNCH(1, 4);
-    else LAUNCH(2, 4);
+    if constexpr (sizeof(T) == 4) {  // bf16 rows that are shared have more than 2560 numbers
+      if (nv == 1) LAUNCH(1, 4);
+    }
+    if (nv == 2) LAUNCH(2, 4);
   } else if (nv == 1) LAUNCH(1, 1);
   else if (nv == 2) LAUNCH(2, 1);
   else if (nv == 3) LAUNCH(3, 1);
