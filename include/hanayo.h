@@ -283,10 +283,10 @@ int hanayo_chunk_adam_step(const hanayo_adam* o, const hanayo_chunk_desc* d, voi
  * the update (hanayo_adam_step_clipped, hanayo_chunk_adam_step_clipped), which saves that pass.  Nothing waits
  * for the device.
  *   norm = sqrt(sumsq[0] + .. + sumsq[parts - 1]);  scale = norm > max_norm ? max_norm / norm : 1
- * Squares are formed and added in 64 bits, so no fp32 gradient is too large or too small for them; the order is fixed and
- * results repeat bit for bit.  A norm that is infinite or NaN (a gradient was): hanayo_op_grad_clip takes scale
- * = 1, and the clipped updates leave parameters and moments as they are and count in `skipped`; either way `norm` shows it.  (A finite
- * norm beyond fp32's range, 3.4e38, is infinite in `norm` alone.)
+ * Squares are formed and added in 64 bits, so no fp32 gradient is too large or too small for them; the order is fixed by the sizes and
+ * by where the tensors lie modulo 16 bytes, and results repeat bit for bit.  A norm that is infinite or NaN (a gradient was):
+ * hanayo_op_grad_clip takes scale = 1, and the clipped updates leave parameters and moments as they are and count in `skipped`;
+ * either way `norm` shows it.  (A finite norm beyond fp32's range, 3.4e38, is infinite in `norm` alone.)
  * ------------------------------------------------------------------------- */
 typedef struct hanayo_grad {
   const void* grad; /* device, fp32 or bf16, on an element's boundary; may be NULL if count is 0 */
@@ -729,6 +729,7 @@ typedef struct hanayo_residual_desc {
 int hanayo_op_residual_forward(const hanayo_residual_desc* d, const void* x, const void* branch, const void* gate,
                                const void* post, const void* pre, void* x_out, void* h, float* stats, void* hip_stream);
 /*
+ *   x_out, stats  as forward left them: the normed row is formed again from x_out as it is stored
  *   dh         device [rows][H], gradient w.r.t. h (NULL without pre_norm)
  *   dx_out     device [rows][H], gradient that reaches x_out from elsewhere; NULL = none (with pre_norm only)
  *   dx, dbranch  device [rows][H], written; dx may be dx_out, no other two tensors may overlap

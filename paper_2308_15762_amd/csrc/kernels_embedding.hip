@@ -4,9 +4,9 @@
 //
 // Both are bound by HBM where they are large and by their launches where they are small.  The gradient first sorts the rows by
 // token (ties in row order), so that the rows of a token follow each other and are added in a fixed order without
-// atomics, whatever the distribution of the tokens.  MI355X, bf16: lookup of 4096 rows of 1024 4.0 us; gradient of 65521 such rows, a
-// quarter of them padding, 30592 tokens, written whole: sort 24 us in four launches, sums and clearing 47.7 us (226 MB, 4.7 TB/s; rows in
-// random order alone cost 13 % of a copy's rate), borders 6.9 us.
+// atomics, whatever the distribution of the tokens.  MI355X, bf16: lookup of 4096 rows of 1024 4.0 us; 65521 rows 44.3 us (fp32 93.9);
+// gradient of 65521 such rows, a quarter of them padding, 30592 tokens, written whole: sort 24 us in four launches, sums and clearing 47 us
+// (226 MB, 4.8 TB/s; rows in random order alone cost 13 % of a copy's rate), borders 6.9 us.
 #include "device_util.h"
 #include "kernels.h"
 
@@ -526,8 +526,10 @@ int embedding_direct(const int32_t* tokens, const void* dout, float scale, float
 // 15.5 us against 25.5 with the radix sort, 8192 rows 22.6 against 30.8, 12288 rows 30.0 against 32.1).
 constexpr int kRankRows = 12288;
 
-// Rows of a piece: enough pieces for four wavefronts on every SIMD where the rows allow it (whole call, 65521 rows of 1024,
-// table written: 16 rows 76.8 us, 8 rows 77.9, 32 rows 85, 64 rows 98; 4096 rows, added: 8 rows 17.5, 16 rows 20.2, 32 rows 27.8).
+// Rows of a piece: as many as leave 4096 pieces, two workgroups of eight for every CU; eight rows where there are too few (whole call, 65521
+// rows of 1024, table written: 16 rows 76.8 us, 8 rows 77.9, 32 rows 85, 64 rows 98; 4096 rows, added: 8 rows 17.5, 16 rows 20.2, 32 rows
+// 27.8).  Two workgroups of the written form (115 registers) fit a CU together, one of the added form (bf16: 180 registers).  4096 rows of 1024 are
+// 128 workgroups: half of the CUs have none.
 int piece_rows(int rows, int H) {
   const long slabs = (H + 511) / 512;
   for (int r = 64; r > 8; r /= 2)

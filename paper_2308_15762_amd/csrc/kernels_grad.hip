@@ -7,7 +7,8 @@
 // and added in 64 bits: the largest and smallest fp32 gradients neither overflow nor vanish, and 2^40 of them add up with
 // an error far below the fp32 result's last bit; the pass reads 4 bytes per conversion and addition, which the 64-bit rate of the vector
 // units covers many times over.  Tensors are cut into tiles, and a launch's tiles go round its workgroups in turn; which
-// partial sum holds what depends on the sizes alone, and the partial sums are added in order, so results repeat bit for bit.
+// partial sum holds what depends on the sizes, and inside a tile on where the tensor lies modulo 16 bytes; the partial sums are added
+// in order.  So results repeat bit for bit for tensors that stay where they are, and may differ in the last of 53 bits where they do not.
 #include <type_traits>
 
 #include "clip.h"
@@ -23,9 +24,9 @@ constexpr unsigned kTileBytes = 32768;  // of a tensor: eight 16-byte loads a th
 constexpr int kMaxBlocks = 2048;        // workgroups of a launch at most: 8 on every CU, one partial sum each
 constexpr int kLoads = kTileBytes / 16 / 256;
 // The pass that forms the norm leaves the first 192 MiB of a call's tensors in the 256 MB cache and reads the rest past it, so that the pass
-// that scales or uses them finds that part there; that pass reads and writes past the cache.  Norm and clipping of 403 MB:
-// 181 us, of 1013 us with Adam on 609 MB (30 bytes an element) 852; with ordinary loads and stores everywhere 238 and 1046, the rest past the
-// cache in the first pass only 200 and 1043, nothing kept 214 and 1013.
+// that scales or uses them finds that part there; that pass reads and writes past the cache.  Variants in turn on one card,
+// norm and clipping of 403 MB / norm and Adam on 609 MB (30 bytes an element): 181 / 852 us; with ordinary loads and stores everywhere
+// 238 / 1046, the rest past the cache in the first pass only 200 / 1043, nothing kept 214 / 1013.  Cards differ: others take 185 / 924 to 937.
 constexpr unsigned kKeepTiles = 192u * (1 << 20) / kTileBytes;
 
 // Up to so many tiles one workgroup forms the sum alone, without the launch that adds up partial sums (norm and clipping of one fp32 tensor,

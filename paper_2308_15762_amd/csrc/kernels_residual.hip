@@ -9,9 +9,10 @@
 //   dx = x_scale D,   dbranch = rstd (b - <b> - fhat <b fhat>),  b = q gamma_post
 //   d_pre  = sum over rows of dh xhat, dh;   d_post = of q fhat, q;   dgate = branch_scale D u (per channel: summed over rows)
 //
-// Everything streams its [rows][H] tensors once and is bound by HBM.  MI355X, bf16: 4096 rows of 1024 forward 8.3 us (34 MB),
-// backward 17.0 us (50 MB; 4 of them the finaliser); 8192 rows of 4096 with a gate per element backward 107 us (537 MB, 5.0 TB/s, what
-// a large copy reaches).
+// Everything streams its [rows][H] tensors once and is bound by HBM.  MI355X, bf16, calls one behind another: 4096 rows of 1024
+// forward 8.3 us (34 MB), backward 17.0 us (50 MB); 8192 rows of 4096 with a gate per element backward 107 us (537 MB, 5.0 TB/s, what
+// a large copy reaches).  A kernel by itself takes longer than its share of that, since starting and draining do not overlap with a
+// neighbour's: 9.5 us, and 15.1 with 3.9 for the finaliser.
 #include "device_util.h"
 #include "kernels.h"
 
@@ -401,6 +402,9 @@ int residual_forward_t(const ResidualArgs& a, hipStream_t stream) {
 // Rows that a workgroup of the backward pass walks at a time, RS wavefronts each.  With a pre-norm a wavefront needs more than the 128
 // registers that sixteen on a CU have: eight (8192 rows of 4096, bf16, RMS norms and a gate per element: 107 us against 157 with
 // sixteen and what does not fit in memory; 4096 rows of 1024: 17.0 against 21.8); without one sixteen (fp32, 1527 rows of 2560: 18.1 against 19.7).
+// Rows that 3, 5, 6 or 7 wavefronts share leave some of the eight out (6, 5, 6, 7 of them).  16.8 M numbers, LayerNorm and RMSNorm, a gate per
+// channel, us in bf16 / fp32: 1024 columns 46.3 / 82.0, 1536 47.9 / 83.2, 2048 46.8 / 83.8, 2560 52.1 / 83.0, 3584 48.8 / 86.6, 4096 49.1 / 87.1
+// (4.3 / 4.9 TB/s at 1024, 3.9 / 4.9 at 2560); a second workgroup on a CU, for which there are registers at 5, is not tried.
 constexpr int row_groups(bool pre, int rs) { return (pre ? 8 : 16) / rs; }
 int backward_blocks(bool pre, int rows, int H) {
   const int rg = row_groups(pre, (H + 511) / 512), blocks = (rows + rg - 1) / rg;
